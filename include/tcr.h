@@ -208,6 +208,88 @@ tcr_status tcr_reduce(const void *in, float *out, uint64_t n, void *stream);
 tcr_status tcr_scan(const void *in, float *out, uint64_t n, void *stream);
 
 /*
+ * Linear attention with a decay for each head: running sums of outer products, restarted for every sequence.
+ *   S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T        (dk x dv, binary32; S before the first token is `state`, or 0)
+ *   out_t = scale * q_t^T S_t
+ * tcr_attention says what the arrays hold.  q, k, v and out hold one row of dk (q, k) or dv (v, out) consecutive elements for
+ * every token and head, of the type `dtype` (TCR_F16 or TCR_BF16); row (sequence b, token t, head h) starts b * stride[0] +
+ * t * stride[1] + h * stride[2] ELEMENTS behind the pointer, in any order of the axes.  Query heads share keys and values:
+ * head h goes with key/value head h / (heads / kv_heads).
+ *   offsets == NULL: `sequences` sequences of `tokens` tokens each.
+ *   otherwise: sequences packed behind one another, sequence b the tokens [offsets[b], offsets[b + 1]) of `tokens` in all
+ *   (stride[0] is not used); offsets is a DEVICE pointer to sequences + 1 non-decreasing token indices as in the irregular calls
+ *   above, not validated either.  Rows of out whose token lies in no sequence are set to 0.
+ * log_decay: DEVICE pointer to `heads` floats, the natural logarithm of what is kept of S from one token to the next (0: all
+ * of it, minus infinity: nothing).
+ * state, final_state: DEVICE pointers, 16-byte aligned, sequences x heads x dk x dv floats each, contiguous; the state in front
+ * of the first token and behind the last (of an empty sequence: the same).  NULL: zeros, and not wanted.  They must be different arrays.
+ * dk and dv: multiples of 8 from 8 to 256; fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED otherwise).  The magnitude of
+ * scale lies between 1e-18 and 1e18.  As everywhere, inputs are finite: an infinity or NaN poisons its own sequence, also up to
+ * 63 tokens in front of it.
+ */
+typedef enum {
+    TCR_F16 = 0,               /* IEEE binary16 */
+    TCR_BF16 = 1,              /* bfloat16 */
+    TCR_F32 = 2,               /* IEEE binary32 */
+    TCR_E4M3 = 3,              /* 8-bit floating point, 4 bits of exponent, 3 of fraction, no infinities (largest value 448) */
+    TCR_I8 = 4                 /* whole numbers from -127 to 127 */
+} tcr_dtype;
+
+typedef struct {
+    uint32_t dtype, heads, kv_heads, dk, dv;
+    uint64_t sequences, tokens;
+    const uint64_t *offsets;
+    const float *log_decay;
+    float scale;
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+} tcr_attention;
+
+tcr_status tcr_linear_attention(const tcr_attention *shape, const void *q, const void *k, const void *v, void *out, const float *state,
+                                float *final_state, void *stream);
+/* One token for every sequence (tokens == 1, offsets == NULL): out and the states behind it.  new_state may be `state`. */
+tcr_status tcr_linear_attention_step(const tcr_attention *shape, const void *q, const void *k, const void *v, void *out, const float *state,
+                                     float *new_state, void *stream);
+/*
+ * Gradients of tcr_linear_attention.  dout is laid out by o_stride; dq, dk, dv are contiguous (sequence, token, head, element
+ * -- packed: token, head, element), dk and dv summed over the heads that share them.  state: the forward call's;
+ * dfinal: the gradient of its final_state (NULL: none); dstate: the gradient of `state` (NULL: not wanted), not dfinal's array.
+ * The decays are constants of a model and have no gradient here.  Where heads share keys and values the call needs tokens *
+ * heads * max(dk, dv) floats of workspace.
+ */
+tcr_status tcr_linear_attention_backward(const tcr_attention *shape, const void *dout, const void *q, const void *k, const void *v, void *dq, void *dk,
+                                         void *dv, const float *state, const float *dfinal, float *dstate, void *stream);
+
+/*
+ * Root-mean-square norm of every row, with the addition in front of it:
+ *   total = x + residual,   rstd = 1 / sqrt(mean(total^2) + eps),   out = total * rstd * weight.
+ * x, residual: rows of cols consecutive elements, x_stride (residual_stride) elements from one row to the next; out, total:
+ * rows x cols, contiguous; weight: cols elements.  x, residual, total and out have the type dtype (TCR_F16, TCR_BF16, TCR_F32),
+ * weight that or TCR_F32; element alignment is enough.  All arithmetic is binary32, rounded once: out comes from the sum before
+ * it is rounded into `total`.  residual == NULL: nothing is added; total, rstd == NULL: not wanted.  total may be the array
+ * of residual or of x (contiguous then).  rstd: `rows` floats, for the gradients.  1 <= cols <= 2^24, rows < 2^31.
+ */
+tcr_status tcr_rms_norm(const void *x, const void *residual, const void *weight, void *out, void *total, float *rstd, uint64_t rows, uint64_t cols,
+                        int64_t x_stride, int64_t residual_stride, float eps, uint32_t dtype, uint32_t weight_dtype, void *stream);
+/*
+ * The same with out in 8 bits: codes (rows x cols bytes, code_type TCR_E4M3 or TCR_I8) and one scale for each `group` columns of
+ * a row (32, 64 or 128, the last group may be shorter; 0: one for the row), scales: rows x ceil(cols / group) floats.
+ *   scale = max|out| / 448 (TCR_I8: 127), at least 2^-126;   code = out / scale, rounded to nearest even.
+ * A row with an infinity or NaN has scales and codes that say so (codes of TCR_I8 are 0 there).
+ */
+tcr_status tcr_rms_norm_quantized(const void *x, const void *residual, const void *weight, void *codes, float *scales, void *total, uint64_t rows,
+                                  uint64_t cols, int64_t x_stride, int64_t residual_stride, float eps, uint32_t dtype, uint32_t weight_dtype,
+                                  uint32_t code_type, uint32_t group, void *stream);
+/*
+ * Gradients of tcr_rms_norm from its `total` (x, where nothing was added) and rstd; dtotal: the gradient of `total`
+ * itself, added to dx (NULL: none).  dx: rows x cols, contiguous, the gradient of x and of residual alike; dweight: cols elements
+ * of the type of weight, the sum over all rows (the same from run to run).  Needs at most 1024 * cols floats of workspace and
+ * runs with cols of them.
+ */
+tcr_status tcr_rms_norm_backward(const void *dout, const void *total, const void *weight, const float *rstd, const void *dtotal, void *dx,
+                                 void *dweight, uint64_t rows, uint64_t cols, int64_t dout_stride, int64_t total_stride, int64_t dtotal_stride,
+                                 uint32_t dtype, uint32_t weight_dtype, void *stream);
+
+/*
  * Bench / test hook: choose among measured alternatives.  Keys and values:
  *   "formulation"  "mfma" (default: matrix-core products) | "dpp" (cross-lane wavefront primitives)
  *   "scan_carry"   "lookback" (default: single pass, decoupled look-back) | "reduce_then_scan" |

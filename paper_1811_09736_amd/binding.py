@@ -30,8 +30,21 @@ EXPORTS = (
     "tcr_irregular_reduce", "tcr_irregular_scan", "tcr_irregular_scan_ex", "tcr_irregular_scan_filled", "tcr_irregular_moments", "tcr_autotune", "tcr_autotune_irregular", "tcr_tuning_export", "tcr_tuning_import",
     "tcr_workspace_bytes", "tcr_set_workspace", "tcr_segmented_moments",
     "tcr_set_variant", "tcr_segmented_scan_noalloc",
+    "tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward",
+    "tcr_rms_norm", "tcr_rms_norm_quantized", "tcr_rms_norm_backward",
     "tcr_kernel_name", "tcr_check_device_flags", "tcr_release", "tcr_release_stream", "tcr_status_string", "tcr_last_hip_error",
 )
+
+
+F16, BF16, F32, E4M3, I8 = range(5)
+_DTYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: E4M3, torch.int8: I8}
+
+
+class AttentionShape(ctypes.Structure):
+    """tcr_attention."""
+    _fields_ = [(n, ctypes.c_uint32) for n in ("dtype", "heads", "kv_heads", "dk", "dv")] + [
+        ("sequences", ctypes.c_uint64), ("tokens", ctypes.c_uint64), ("offsets", ctypes.c_void_p), ("log_decay", ctypes.c_void_p),
+        ("scale", ctypes.c_float)] + [(n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride", "o_stride")]
 
 
 class TcrError(RuntimeError):
@@ -82,6 +95,16 @@ def _load() -> ctypes.CDLL:
     lib.tcr_tuning_import.restype = ctypes.c_int
     lib.tcr_segmented_moments.argtypes = [vp, fp, fp, u64, u64, vp]
     lib.tcr_segmented_moments.restype = ctypes.c_int
+    shape, u32, i64, f32 = ctypes.POINTER(AttentionShape), ctypes.c_uint32, ctypes.c_int64, ctypes.c_float
+    lib.tcr_linear_attention.argtypes = [shape] + [vp] * 7
+    lib.tcr_linear_attention_step.argtypes = [shape] + [vp] * 7
+    lib.tcr_linear_attention_backward.argtypes = [shape] + [vp] * 11
+    lib.tcr_rms_norm.argtypes = [vp] * 6 + [u64, u64, i64, i64, f32, u32, u32, vp]
+    lib.tcr_rms_norm_quantized.argtypes = [vp] * 6 + [u64, u64, i64, i64, f32, u32, u32, u32, u32, vp]
+    lib.tcr_rms_norm_backward.argtypes = [vp] * 7 + [u64, u64, i64, i64, i64, u32, u32, vp]
+    for name in ("tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward", "tcr_rms_norm", "tcr_rms_norm_quantized",
+                 "tcr_rms_norm_backward"):
+        getattr(lib, name).restype = ctypes.c_int
     lib.tcr_workspace_bytes.argtypes = [ctypes.c_int, u64, u64]
     lib.tcr_workspace_bytes.restype = u64
     lib.tcr_set_workspace.argtypes = [vp, u64]
@@ -404,6 +427,184 @@ def segmented_moments(x: torch.Tensor, seg_len: int, stream: Optional[torch.cuda
     q = torch.empty(count, dtype=torch.float32, device=x.device)
     _run(_lib.tcr_segmented_moments, "tcr_segmented_moments", x, stream, x.data_ptr(), a.data_ptr(), q.data_ptr(), n, seg_len)
     return a, q
+
+
+# ------------------------------------------------------------------------------ linear attention with decay, root-mean-square norm
+def _rows_of(x, name: str, dims: int, dtype, like) -> None:
+    if not (x.is_cuda and x.dim() == dims and x.dtype == dtype and x.device == like.device and (x.stride(-1) == 1 or x.shape[-1] == 1)):
+        raise TypeError(f"{name} must be a {dims}-D {dtype} CUDA tensor on q's device whose last dimension is contiguous")
+
+
+def _states_of(x, name: str, shape, like) -> None:
+    if not (x.is_cuda and x.dtype == torch.float32 and x.is_contiguous() and x.device == like.device and tuple(x.shape) == tuple(shape)):
+        raise TypeError(f"{name} must be a contiguous float32 CUDA tensor of shape {tuple(shape)} on q's device")
+
+
+def _strides(x: torch.Tensor):
+    """Sequence, token and head strides of [sequence, token, head, element] or [token, head, element]."""
+    st = x.stride()
+    return (ctypes.c_int64 * 3)(*st[:3]) if len(st) == 4 else (ctypes.c_int64 * 3)(0, *st[:2])
+
+
+def _attention(q, k, v, o, log_decay, scale, offsets, step=False):
+    """The checked tcr_attention of a call; q, k, v, o: [sequence, token, head, element], packed or for one token [token, head,
+    element]."""
+    if not (q.is_cuda and q.dtype in (torch.float16, torch.bfloat16)):
+        raise TypeError("q must be a float16 or bfloat16 CUDA tensor")
+    dims = 4 if offsets is None and not step else 3
+    for x, name in ((q, "q"), (k, "k"), (v, "v"), (o, "out")):
+        _rows_of(x, name, dims, q.dtype, q)
+    heads, kv, dk, dv = q.shape[-2], k.shape[-2], q.shape[-1], v.shape[-1]
+    if not (k.shape[:-2] == q.shape[:-2] and v.shape[:-1] == k.shape[:-1] and k.shape[-1] == dk and tuple(o.shape) == (*q.shape[:-1], dv)
+            and kv and heads % kv == 0):
+        raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, out {tuple(o.shape)}")
+    if not (log_decay.is_cuda and log_decay.dtype == torch.float32 and log_decay.is_contiguous() and tuple(log_decay.shape) == (heads,)
+            and log_decay.device == q.device):
+        raise TypeError(f"log_decay must be a contiguous float32 CUDA tensor of {heads} elements on q's device")
+    if offsets is not None:
+        sequences, tokens = _check_offsets(q, offsets), q.shape[0]
+    elif step:
+        sequences, tokens = q.shape[0], 1
+    else:
+        sequences, tokens = q.shape[:2]
+    strides = [_strides(x) for x in (q, k, v, o)]
+    if step:                                 # the leading axis is the sequence's
+        strides = [(ctypes.c_int64 * 3)(st[1], 0, st[2]) for st in strides]
+    return AttentionShape(_DTYPES[q.dtype], heads, kv, dk, dv, sequences, tokens, None if offsets is None else offsets.data_ptr(),
+                          log_decay.data_ptr(), dk ** -0.5 if scale is None else scale, *strides)
+
+
+def _ptr(x: Optional[torch.Tensor]):
+    return None if x is None else x.data_ptr()
+
+
+def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, scale: Optional[float] = None,
+                     offsets: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None, final_state: bool = False,
+                     out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """tcr_linear_attention: out_t = scale * q_t S_t with S_t = exp(log_decay) S_{t-1} + k_t v_t^T, for every sequence and head.
+
+    q [B, T, H, dk], k [B, T, G, dk], v [B, T, G, dv], H a multiple of G; or packed sequences [N, H, dk] ... with `offsets`
+    ([sequences + 1], int64).  log_decay [H], float32.  scale: dk ** -0.5 if not given.  state [sequences, H, dk, dv], float32: the
+    states to go on from.  Returns out [B, T, H, dv] ([N, H, dv]), with final_state also the states behind the last tokens."""
+    if out is None:
+        out = torch.empty(*q.shape[:-1], v.shape[-1], dtype=q.dtype, device=q.device)
+    shape = _attention(q, k, v, out, log_decay, scale, offsets)
+    states = (shape.sequences, shape.heads, shape.dk, shape.dv)
+    if state is not None:
+        _states_of(state, "state", states, q)
+    last = torch.empty(states, dtype=torch.float32, device=q.device) if final_state else None
+    _run(_lib.tcr_linear_attention, "tcr_linear_attention", q, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+         _ptr(state), _ptr(last))
+    return (out, last) if final_state else out
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor,
+                          scale: Optional[float] = None, new_state: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """tcr_linear_attention_step: one token for every sequence.  q [B, H, dk], k [B, G, dk], v [B, G, dv], state [B, H, dk, dv].
+    The new states go to new_state, without it to `state` itself.  Returns out [B, H, dv]."""
+    if out is None:
+        out = torch.empty(*q.shape[:-1], v.shape[-1], dtype=q.dtype, device=q.device)
+    shape = _attention(q, k, v, out, log_decay, scale, None, step=True)
+    states = (shape.sequences, shape.heads, shape.dk, shape.dv)
+    _states_of(state, "state", states, q)
+    if new_state is None:
+        new_state = state
+    else:
+        _states_of(new_state, "new_state", states, q)
+    _run(_lib.tcr_linear_attention_step, "tcr_linear_attention_step", q, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+         state.data_ptr(), new_state.data_ptr())
+    return out
+
+
+def linear_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                              scale: Optional[float] = None, offsets: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None,
+                              dfinal: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """tcr_linear_attention_backward: (dq, dk, dv, dstate) from dout and, where the final states were used, their gradient dfinal.
+    dstate is None without `state`.  The decays are constants."""
+    shape = _attention(q, k, v, dout, log_decay, scale, offsets)
+    states = (shape.sequences, shape.heads, shape.dk, shape.dv)
+    dstate = None
+    if state is not None:
+        _states_of(state, "state", states, q)
+        dstate = torch.empty(states, dtype=torch.float32, device=q.device)
+    if dfinal is not None:
+        _states_of(dfinal, "dfinal", states, q)
+    dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+    _run(_lib.tcr_linear_attention_backward, "tcr_linear_attention_backward", q, stream, shape, dout.data_ptr(), q.data_ptr(), k.data_ptr(),
+         v.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(state), _ptr(dfinal), _ptr(dstate))
+    return dq, dk, dv, dstate
+
+
+def _norm_rows(x, name: str, like) -> int:
+    """The stride from one row to the next of [..., cols]: the leading axes have to be one."""
+    if not (x.is_cuda and x.dtype == like.dtype and x.shape == like.shape and x.device == like.device and x.dim() >= 1
+            and (x.stride(-1) == 1 or x.shape[-1] == 1)):
+        raise TypeError(f"{name} must be a CUDA tensor of x's shape, type and device whose last dimension is contiguous")
+    if x.dim() == 2 or x.is_contiguous():
+        return x.stride(0) if x.dim() == 2 else x.shape[-1]
+    try:
+        return x.view(-1, x.shape[-1]).stride(0)
+    except RuntimeError:
+        raise TypeError(f"the leading dimensions of {name} must be one dimension with one stride") from None
+
+
+def _norm_input(x, weight):
+    if not (x.is_cuda and x.dtype in (torch.float16, torch.bfloat16, torch.float32) and x.dim() >= 1 and x.shape[-1] >= 1):
+        raise TypeError("x must be a float16, bfloat16 or float32 CUDA tensor [..., cols]")
+    if not (weight.is_cuda and weight.dtype in (x.dtype, torch.float32) and weight.is_contiguous() and tuple(weight.shape) == (x.shape[-1],)
+            and weight.device == x.device):
+        raise TypeError(f"weight must be a contiguous CUDA tensor of {x.shape[-1]} elements of x's type or float32 on x's device")
+    return x.numel() // x.shape[-1], x.shape[-1]
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, rstd: bool = False,
+             stream: Optional[torch.cuda.Stream] = None):
+    """tcr_rms_norm over the last dimension: x * weight / sqrt(mean(x^2) + eps).  With a residual of x's shape, the norm of x +
+    residual: returns (out, x + residual).  With rstd=True the reciprocal root mean square of every row (float32) comes last."""
+    rows, cols = _norm_input(x, weight)
+    xs, rs = _norm_rows(x, "x", x), _norm_rows(residual, "residual", x) if residual is not None else 0
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    total = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual is not None else None
+    root = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd else None
+    _run(_lib.tcr_rms_norm, "tcr_rms_norm", x, stream, x.data_ptr(), _ptr(residual), weight.data_ptr(), out.data_ptr(), _ptr(total), _ptr(root),
+         rows, cols, xs, rs, eps, _DTYPES[x.dtype], _DTYPES[weight.dtype])
+    got = tuple(t for t in (out, total, root) if t is not None)
+    return got if len(got) > 1 else out
+
+
+def rms_norm_quantized(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                       dtype: torch.dtype = torch.float8_e4m3fn, group: int = 0, stream: Optional[torch.cuda.Stream] = None):
+    """tcr_rms_norm_quantized: the norm in 8 bits (float8_e4m3fn or int8) with a scale for each `group` columns (32, 64, 128; 0: for
+    the row): (codes [..., cols], scales [..., groups]), with a residual (codes, scales, x + residual).  codes * scales is the norm."""
+    rows, cols = _norm_input(x, weight)
+    if dtype not in (torch.float8_e4m3fn, torch.int8):
+        raise TypeError("dtype must be torch.float8_e4m3fn or torch.int8")
+    if group not in (0, 32, 64, 128):
+        raise ValueError("group must be 0, 32, 64 or 128")
+    xs, rs = _norm_rows(x, "x", x), _norm_rows(residual, "residual", x) if residual is not None else 0
+    codes = torch.empty(x.shape, dtype=dtype, device=x.device)
+    scales = torch.empty(*x.shape[:-1], -(-cols // group) if group else 1, dtype=torch.float32, device=x.device)
+    total = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual is not None else None
+    _run(_lib.tcr_rms_norm_quantized, "tcr_rms_norm_quantized", x, stream, x.data_ptr(), _ptr(residual), weight.data_ptr(), codes.data_ptr(),
+         scales.data_ptr(), _ptr(total), rows, cols, xs, rs, eps, _DTYPES[x.dtype], _DTYPES[weight.dtype], _DTYPES[dtype], group)
+    return (codes, scales) if total is None else (codes, scales, total)
+
+
+def rms_norm_backward(dout: torch.Tensor, total: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dtotal: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None):
+    """tcr_rms_norm_backward: (dx, dweight) from rms_norm's x + residual (its x, without a residual) and rstd; dtotal: the gradient
+    of x + residual itself, added.  dx is the gradient of x and of the residual alike."""
+    rows, cols = _norm_input(total, weight)
+    ds, ts = _norm_rows(dout, "dout", total), _norm_rows(total, "total", total)
+    ms = _norm_rows(dtotal, "dtotal", total) if dtotal is not None else 0
+    if not (rstd.is_cuda and rstd.dtype == torch.float32 and rstd.is_contiguous() and rstd.numel() == rows and rstd.device == total.device):
+        raise TypeError(f"rstd must be a contiguous float32 CUDA tensor of {rows} elements on the device of total")
+    dx = torch.empty(total.shape, dtype=total.dtype, device=total.device)
+    dweight = torch.empty(cols, dtype=weight.dtype, device=total.device)
+    _run(_lib.tcr_rms_norm_backward, "tcr_rms_norm_backward", total, stream, dout.data_ptr(), total.data_ptr(), weight.data_ptr(), rstd.data_ptr(),
+         _ptr(dtotal), dx.data_ptr(), dweight.data_ptr(), rows, cols, ds, ts, ms, _DTYPES[total.dtype], _DTYPES[weight.dtype])
+    return dx, dweight
 
 
 def workspace_bytes(op: int, n: int, seg_len: int) -> int:

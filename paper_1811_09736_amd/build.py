@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -21,21 +23,30 @@ HIPCC_FLAGS = [
 
 
 def sources():
-    return [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith(".hip")]
+    return [os.path.join(d, f) for d in (CSRC, os.path.join(CSRC, "layers")) for f in sorted(os.listdir(d)) if f.endswith(".hip")]
 
 
 def build_library(verbose: bool = False) -> str:
+    """One object per source, side by side, and the library from them."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + ["-o", LIB_PATH] + sources()
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    # the host pass does not know the device-only target feature and says so; that is harmless
-    out = "\n".join(l for l in proc.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out, flush=True)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        # the host pass does not know the device-only target feature and says so; that is harmless
+        out = "\n".join(l for l in proc.stdout.splitlines() if "packed-fp32-ops" not in l)
+        if proc.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + out)
+        if verbose and out.strip():
+            print(out, flush=True)
+
+    with tempfile.TemporaryDirectory() as work:
+        objects = [os.path.join(work, os.path.basename(s) + ".o") for s in sources()]
+        compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+        with ThreadPoolExecutor(max_workers=4) as pool:
+            list(pool.map(run, ([hipcc] + compile_flags + ["-c", "-o", o, s] for s, o in zip(sources(), objects))))
+        run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB_PATH] + objects)
     return LIB_PATH
 
 

@@ -1,0 +1,412 @@
+// Root-mean-square norm with the residual's addition: one pass, the row in registers between its sum of squares and its use.
+//
+//     s = x + r,   rstd = 1 / sqrt(mean s^2 + eps),   y = s rstd w
+// and y in the type of x, or in 8 bits with a scale for each row or each group of columns:
+//     scale = max |y| / M (M = 448 for e4m3, 127 for whole numbers; at least 2^-126),   code = y / scale, rounded to nearest even.
+// Everything between the loads and the stores is binary32; s is stored rounded to the type of x, y comes from the sum before
+// that rounding.
+//
+// Gradients, with g = dy w:   dx = rstd (g - s rstd^2 mean(g s)) + ds,   dw = sum over rows of dy s rstd.
+#pragma once
+#include "tcr_shared.hpp"
+
+namespace tcr {
+namespace layers {
+
+constexpr int kVec = 8;                        // elements a lane loads at once: 16 bytes of 16-bit types
+constexpr float kSmallestScale = 1.17549435e-38f;
+
+enum NormOut { kNormSame = 0, kNormE4M3 = 1, kNormI8 = 2 };
+
+struct Norm {
+    const void *x, *residual, *weight;
+    void *out, *total;
+    float *scales, *rstd;
+    uint64_t rows, cols;
+    int64_t x_stride, r_stride;
+    float eps;
+    uint32_t group;                            // columns per scale; 0: the row
+    uint32_t weight_wide;                      // weight in binary32 beside inputs of 16 bits
+};
+
+struct NormGrad {
+    const void *dout, *total, *weight, *dtotal;
+    const float* rstd;
+    void *dx, *dweight;
+    float* part;                               // [parts][cols] sums of dweight
+    uint64_t rows, cols;
+    int64_t dout_stride, total_stride, dtotal_stride;
+    uint32_t weight_wide, parts;
+};
+
+// Vectors of kVec elements that need no more alignment than an element.
+template <typename T> struct Vec;
+template <> struct Vec<_Float16> { typedef _Float16 v __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Vec<__bf16> { typedef __bf16 v __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Vec<float> { typedef float v __attribute__((ext_vector_type(8), aligned(4))); };
+
+// Columns col .. col + 7 of a row, 0 beyond its end.
+template <typename T>
+__device__ __forceinline__ void load_vec(const T* row, uint64_t col, uint64_t cols, float (&v)[kVec]) {
+    if (col + kVec <= cols) {
+        const typename Vec<T>::v x = *reinterpret_cast<const typename Vec<T>::v*>(row + col);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = (float)x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = col + i < cols ? (float)row[col + i] : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_vec(T* row, uint64_t col, uint64_t cols, const float (&v)[kVec]) {
+    if (col + kVec <= cols) {
+        typename Vec<T>::v x;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x[i] = (T)v[i];
+        *reinterpret_cast<typename Vec<T>::v*>(row + col) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (col + i < cols) row[col + i] = (T)v[i];
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load_weight(const void* w, uint32_t wide, uint64_t col, uint64_t cols, float (&v)[kVec]) {
+    if (wide) load_vec(static_cast<const float*>(w), col, cols, v);
+    else load_vec(static_cast<const T*>(w), col, cols, v);
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    return x;
+}
+// The larger magnitude; NaN, whose bits are the largest, stays.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_largest(uint32_t x) {
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) x = larger(x, (uint32_t)__shfl_xor((int)x, m));
+    return x;
+}
+// The sum (maximum) over the WAVES wavefronts of a workgroup, each wavefront's own given.  `sums` is free again only after the
+// next barrier.
+template <int WAVES>
+__device__ __forceinline__ float block_sum(float x, float* sums) {
+    x = wave_sum(x);
+    if constexpr (WAVES == 1) return x;
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total += sums[w];
+    return total;
+}
+template <int WAVES>
+__device__ __forceinline__ uint32_t block_largest(uint32_t x, uint32_t* most) {
+    x = lanes_largest<64>(x);
+    if constexpr (WAVES == 1) return x;
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = x;
+    __syncthreads();
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all = larger(all, most[w]);
+    return all;
+}
+
+template <int OUT>
+__device__ __forceinline__ float scale_of(uint32_t largest) {
+    const float top = __builtin_bit_cast(float, largest) / (OUT == kNormE4M3 ? 448.0f : 127.0f);
+    return top < kSmallestScale ? kSmallestScale : top;          // (NaN stays)
+}
+// Eight codes.  |y / scale| is at most M but for a rounding, so nothing has to be cut off.  NaN becomes NaN, or 0 as a whole number.
+template <int OUT>
+__device__ __forceinline__ u2v codes_of(const float (&y)[kVec], float inverse) {
+    u2v c;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const float a = y[4 * half] * inverse, b = y[4 * half + 1] * inverse, d = y[4 * half + 2] * inverse, e = y[4 * half + 3] * inverse;
+        if constexpr (OUT == kNormE4M3) {
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+            c[half] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(d, e, w, true);
+        } else {
+            auto whole = [](float v) { return (uint32_t)(uint8_t)(int8_t)(v == v ? (int)rintf(v) : 0); };
+            c[half] = whole(a) | whole(b) << 8 | whole(d) << 16 | whole(e) << 24;
+        }
+    }
+    return c;
+}
+__device__ __forceinline__ void store_codes(uint8_t* row, uint64_t col, uint64_t cols, u2v c) {
+    if (col + kVec <= cols) {
+        typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(1)));
+        *reinterpret_cast<pair*>(row + col) = c;
+    } else {
+        for (int i = 0; i < kVec; ++i)
+            if (col + i < cols) row[col + i] = (uint8_t)(c[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+// WAVES wavefronts per row, ITEMS vectors per lane: rows of up to WAVES * 64 * ITEMS * 8 columns.
+template <typename T, int OUT, int WAVES, int ITEMS>
+__global__ __launch_bounds__(WAVES * 64) void norm_kernel(const Norm a) {
+    constexpr int kLanes = WAVES * 64;
+    __shared__ float sums[WAVES];
+    __shared__ uint32_t most[WAVES];
+    const uint64_t row = blockIdx.x, cols = a.cols;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
+    const T* r = a.residual != nullptr ? static_cast<const T*>(a.residual) + (int64_t)row * a.r_stride : nullptr;
+
+    float s[ITEMS][kVec];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) load_vec(x, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, s[i]);
+    if (r != nullptr) {
+        float add[ITEMS][kVec];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) load_vec(r, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, add[i]);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) s[i][j] += add[i][j];
+    }
+    float square = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) square = fmaf(s[i][j], s[i][j], square);
+    const float rstd = 1.0f / sqrtf(block_sum<WAVES>(square, sums) / (float)cols + a.eps);
+    if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
+    if (a.total != nullptr) {
+        T* total = static_cast<T*>(a.total) + row * cols;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) store_vec(total, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, s[i]);
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+        float w[kVec];
+        load_weight<T>(a.weight, a.weight_wide, col, cols, w);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            s[i][j] = s[i][j] * rstd * w[j];
+            if constexpr (OUT != kNormSame) top = larger(top, magnitude(s[i][j]));
+        }
+        if constexpr (OUT == kNormSame) {
+            store_vec(static_cast<T*>(a.out) + row * cols, col, cols, s[i]);
+        } else if (a.group != 0) {
+            // 4, 8 or 16 lanes hold a group (the row starts on a group, and lanes beyond its end hold zeros)
+            uint32_t g = lanes_largest<4>(top);
+            if (a.group >= 64) g = larger(g, (uint32_t)__shfl_xor((int)g, 4));
+            if (a.group >= 128) g = larger(g, (uint32_t)__shfl_xor((int)g, 8));
+            const float scale = scale_of<OUT>(g);
+            if (col < cols) {
+                store_codes(static_cast<uint8_t*>(a.out) + row * cols, col, cols, codes_of<OUT>(s[i], 1.0f / scale));
+                if (col % a.group == 0) a.scales[row * ((cols + a.group - 1) / a.group) + col / a.group] = scale;
+            }
+            top = 0;
+        }
+    }
+    if constexpr (OUT != kNormSame) {
+        if (a.group == 0) {
+            const float scale = scale_of<OUT>(block_largest<WAVES>(top, most));
+            if (threadIdx.x == 0) a.scales[row] = scale;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+                if (col < cols) store_codes(static_cast<uint8_t*>(a.out) + row * cols, col, cols, codes_of<OUT>(s[i], 1.0f / scale));
+            }
+        }
+    }
+}
+
+// Rows that no registers hold: the row is read again for each use (from a cache, mostly).
+constexpr int kLongWaves = 16;
+template <typename T, int OUT>
+__global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a) {
+    constexpr uint64_t kStep = kLongWaves * 64 * kVec;
+    __shared__ float sums[kLongWaves];
+    __shared__ uint32_t most[kLongWaves];
+    const uint64_t row = blockIdx.x, cols = a.cols;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
+    const T* r = a.residual != nullptr ? static_cast<const T*>(a.residual) + (int64_t)row * a.r_stride : nullptr;
+    auto sum_at = [&](uint64_t col, float(&s)[kVec]) {
+        load_vec(x, col, cols, s);
+        if (r == nullptr) return;
+        float add[kVec];
+        load_vec(r, col, cols, add);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) s[j] += add[j];
+    };
+    float square = 0.0f, s[kVec], w[kVec];
+    for (uint64_t col = threadIdx.x * kVec; col < cols; col += kStep) {
+        sum_at(col, s);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) square = fmaf(s[j], s[j], square);
+    }
+    const float rstd = 1.0f / sqrtf(block_sum<kLongWaves>(square, sums) / (float)cols + a.eps);
+    if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
+    float scale = 1.0f;
+    if constexpr (OUT != kNormSame) {
+        if (a.group == 0) {
+            uint32_t top = 0;
+            for (uint64_t col = threadIdx.x * kVec; col < cols; col += kStep) {
+                sum_at(col, s);
+                load_weight<T>(a.weight, a.weight_wide, col, cols, w);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) top = larger(top, magnitude(s[j] * rstd * w[j]));
+            }
+            scale = scale_of<OUT>(block_largest<kLongWaves>(top, most));
+            if (threadIdx.x == 0) a.scales[row] = scale;
+        }
+    }
+    // (all lanes of a wavefront take every step: a group's lanes have to be there together.  `total` may be `residual`: each
+    // lane reads its columns for the last time right before it writes them.)
+    for (uint64_t first = 0; first < cols; first += kStep) {
+        const uint64_t col = first + threadIdx.x * kVec;
+        sum_at(col, s);
+        if (a.total != nullptr) store_vec(static_cast<T*>(a.total) + row * cols, col, cols, s);
+        load_weight<T>(a.weight, a.weight_wide, col, cols, w);
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            s[j] = s[j] * rstd * w[j];
+            if constexpr (OUT != kNormSame) top = larger(top, magnitude(s[j]));
+        }
+        if constexpr (OUT == kNormSame) {
+            store_vec(static_cast<T*>(a.out) + row * cols, col, cols, s);
+        } else {
+            if (a.group != 0) {
+                uint32_t g = lanes_largest<4>(top);
+                if (a.group >= 64) g = larger(g, (uint32_t)__shfl_xor((int)g, 4));
+                if (a.group >= 128) g = larger(g, (uint32_t)__shfl_xor((int)g, 8));
+                scale = scale_of<OUT>(g);
+                if (col < cols && col % a.group == 0) a.scales[row * ((cols + a.group - 1) / a.group) + col / a.group] = scale;
+            }
+            if (col < cols) store_codes(static_cast<uint8_t*>(a.out) + row * cols, col, cols, codes_of<OUT>(s, 1.0f / scale));
+        }
+    }
+}
+
+// Gradients: a workgroup takes every parts-th row and keeps its sums of dweight in registers.
+template <typename T, int WAVES, int ITEMS>
+__global__ __launch_bounds__(WAVES * 64) void norm_grad_kernel(const NormGrad a) {
+    constexpr int kLanes = WAVES * 64;
+    __shared__ float sums[2][WAVES];
+    const uint64_t cols = a.cols;
+    float dw[ITEMS][kVec] = {};
+    int turn = 0;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += a.parts, turn ^= 1) {
+        const T* dy = static_cast<const T*>(a.dout) + (int64_t)row * a.dout_stride;
+        const T* total = static_cast<const T*>(a.total) + (int64_t)row * a.total_stride;
+        const float rstd = a.rstd[row];
+        float g[ITEMS][kVec], s[ITEMS][kVec], dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+            load_vec(dy, col, cols, g[i]);
+            load_vec(total, col, cols, s[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+            float w[kVec];
+            load_weight<T>(a.weight, a.weight_wide, col, cols, w);
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                dw[i][j] = fmaf(g[i][j] * rstd, s[i][j], dw[i][j]);
+                g[i][j] *= w[j];
+                dot = fmaf(g[i][j], s[i][j], dot);
+            }
+        }
+        // (two places for the sums: a wavefront that is a row ahead writes to the other one)
+        const float c = block_sum<WAVES>(dot, sums[turn]) / (float)cols * rstd * rstd;
+        T* dx = static_cast<T*>(a.dx) + row * cols;
+        const T* more = a.dtotal != nullptr ? static_cast<const T*>(a.dtotal) + (int64_t)row * a.dtotal_stride : nullptr;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+            float add[kVec] = {};
+            if (more != nullptr) load_vec(more, col, cols, add);
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) g[i][j] = fmaf(rstd, g[i][j] - s[i][j] * c, add[j]);
+            store_vec(dx, col, cols, g[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) store_vec(a.part + (uint64_t)blockIdx.x * cols, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, dw[i]);
+}
+
+// The same for rows that no registers hold: dx here, dweight in norm_weight_kernel.
+template <typename T>
+__global__ __launch_bounds__(kLongWaves * 64) void norm_grad_long_kernel(const NormGrad a) {
+    constexpr uint64_t kStep = kLongWaves * 64 * kVec;
+    __shared__ float sums[kLongWaves];
+    const uint64_t row = blockIdx.x, cols = a.cols;
+    const T* dy = static_cast<const T*>(a.dout) + (int64_t)row * a.dout_stride;
+    const T* total = static_cast<const T*>(a.total) + (int64_t)row * a.total_stride;
+    const T* more = a.dtotal != nullptr ? static_cast<const T*>(a.dtotal) + (int64_t)row * a.dtotal_stride : nullptr;
+    const float rstd = a.rstd[row];
+    float g[kVec], s[kVec], w[kVec], dot = 0.0f;
+    auto load = [&](uint64_t col) {
+        load_vec(dy, col, cols, g);
+        load_vec(total, col, cols, s);
+        load_weight<T>(a.weight, a.weight_wide, col, cols, w);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) g[j] *= w[j];
+    };
+    for (uint64_t col = threadIdx.x * kVec; col < cols; col += kStep) {
+        load(col);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) dot = fmaf(g[j], s[j], dot);
+    }
+    const float c = block_sum<kLongWaves>(dot, sums) / (float)cols * rstd * rstd;
+    for (uint64_t col = threadIdx.x * kVec; col < cols; col += kStep) {
+        load(col);
+        float add[kVec] = {};
+        if (more != nullptr) load_vec(more, col, cols, add);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) g[j] = fmaf(rstd, g[j] - s[j] * c, add[j]);
+        store_vec(static_cast<T*>(a.dx) + row * cols, col, cols, g);
+    }
+}
+
+// Sums of dweight over every parts-th row, for 512 columns a workgroup (rows that no registers hold).
+template <typename T>
+__global__ __launch_bounds__(64) void norm_weight_kernel(const NormGrad a) {
+    const uint64_t tiles = (a.cols + 64 * kVec - 1) / (64 * kVec), col = (blockIdx.x % tiles * 64 + threadIdx.x) * kVec;
+    const uint32_t part = (uint32_t)(blockIdx.x / tiles);
+    float dw[kVec] = {};
+    for (uint64_t row = part; row < a.rows; row += a.parts) {
+        float g[kVec], s[kVec];
+        load_vec(static_cast<const T*>(a.dout) + (int64_t)row * a.dout_stride, col, a.cols, g);
+        load_vec(static_cast<const T*>(a.total) + (int64_t)row * a.total_stride, col, a.cols, s);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) dw[j] = fmaf(g[j] * a.rstd[row], s[j], dw[j]);
+    }
+    store_vec(a.part + (uint64_t)part * a.cols, col, a.cols, dw);
+}
+
+// dweight from the parts: 64 columns a workgroup, the parts among its 16 wavefronts.
+template <typename OUT>
+__global__ __launch_bounds__(1024) void norm_parts_kernel(const float* __restrict__ part, OUT* __restrict__ dweight, uint64_t cols, uint32_t parts) {
+    __shared__ float sums[16][64];
+    const uint64_t col = (uint64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    const int wave = threadIdx.x >> 6;
+    float sum = 0.0f;
+    if (col < cols) {
+#pragma unroll 8
+        for (uint32_t p = wave; p < parts; p += 16) sum += part[(uint64_t)p * cols + col];
+    }
+    sums[wave][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (wave == 0 && col < cols) {
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) sum += sums[w][threadIdx.x];
+        dweight[col] = (OUT)sum;
+    }
+}
+
+}  // namespace layers
+}  // namespace tcr

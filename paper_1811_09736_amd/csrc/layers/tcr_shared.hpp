@@ -1,0 +1,38 @@
+// What the operators in this directory use of the library's host side (defined in tcr_api.hip): the workspace of a stream and
+// the text of the last HIP error; and the checks and loads that they share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../../include/tcr.h"
+
+namespace tcr {
+namespace host {
+
+// Room for `want` floats in the workspace that calls on `stream` use (a multiple of 256 bytes, aligned to 256 bytes), or for
+// fewer where it cannot be grown -- the caller's buffer, a stream that is being recorded: *got says how many, at most `want`.
+// The memory belongs to the calls on the stream in their order, as all of the workspace does.
+tcr_status partials_for(hipStream_t stream, uint64_t want, float** room, uint64_t* got);
+
+// TCR_OK, or TCR_ERR_HIP with the error's text kept for tcr_last_hip_error.
+tcr_status launched(const char* what);
+
+}  // namespace host
+
+namespace layers {
+
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
+typedef float f4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+
+inline bool on_boundary(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline uint64_t div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+template <typename T> struct Bits;
+template <> struct Bits<_Float16> { typedef half8v v8; };
+template <> struct Bits<__bf16> { typedef bf8v v8; };
+
+}  // namespace layers
+}  // namespace tcr

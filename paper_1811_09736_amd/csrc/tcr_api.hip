@@ -1,9 +1,31 @@
 // C ABI of the library (declared in include/tcr.h), part 3 of 3 of the host side: argument validation and
 // the exported entry points.  The workspace lives in tcr_workspace.hpp, the dispatch in tcr_dispatch.hpp.
 #include "tcr_dispatch.hpp"
+#include "layers/tcr_shared.hpp"
 
 using namespace tcr;
 using namespace tcr::host;
+
+// ------------------------------------------------------------------------------ for the operators in layers/
+tcr_status tcr::host::partials_for(hipStream_t stream, uint64_t want, float** room, uint64_t* got) {
+    *room = nullptr;
+    *got = 0;
+    if (want == 0) return TCR_OK;
+    Workspace* ws = nullptr;
+    bool capturing = false;
+    tcr_status st = get_workspace(stream, &ws, &capturing);
+    if (st != TCR_OK) return st;
+    const uint64_t most = partials_limit(ws, capturing);
+    if (want > most) want = most;
+    if (want == 0) return TCR_OK;
+    st = ensure_partials(ws, stream, want, capturing);
+    if (st != TCR_OK) return st;
+    *room = ws->partials;
+    *got = want;
+    return TCR_OK;
+}
+
+tcr_status tcr::host::launched(const char* what) { return check_launch(what); }
 
 // ================================================================================ C ABI
 
