@@ -1,5 +1,6 @@
 // Host side of linear attention with a decay for each head: checks, roles, which kernels run.
 #include "tcr_attention.hpp"
+#include "tcr_attention_chunk.hpp"
 
 #include <cmath>
 #include <exception>
@@ -53,15 +54,13 @@ Scan scan_of(const tcr_attention& a, const View& va, const View& vb, const View&
     return s;
 }
 
+// Tokens of a sequence up to which its states stay in registers from token to token: a step costs 1.2 us, a chunk's fixed cost is 10 us.
+constexpr uint64_t kStepTokens = 8;
+constexpr uint64_t kFill = 512;                    // workgroups that fill the chip: two on each compute unit
+
 template <typename T, typename OUT>
-tcr_status run(const Scan& a, hipStream_t stream) {
+tcr_status run_steps(const Scan& a, hipStream_t stream) {
     const uint64_t pairs = a.sequences * a.heads;
-    if (a.offsets != nullptr && a.total != 0) {
-        attention_outside_kernel<OUT><<<dim3((unsigned)div_up(a.total, 64)), dim3(256), 0, stream>>>(a);
-        const tcr_status st = launched("attention_outside_kernel");
-        if (st != TCR_OK) return st;
-    }
-    if (pairs == 0) return TCR_OK;
     if (pairs * div_up(a.dv, 64) >= 1024)
         attention_step_kernel<T, 16, OUT><<<dim3((unsigned)(pairs * div_up(a.dv, 64))), dim3(kStepThreads), 0, stream>>>(a);
     else
@@ -69,10 +68,99 @@ tcr_status run(const Scan& a, hipStream_t stream) {
     return launched("attention_step_kernel");
 }
 
+// The kernel that takes a pair of widths: rows and columns of S that a workgroup holds, tokens of a chunk.
+struct ChunkShape {
+    uint32_t rows, cols, chunk;
+};
+ChunkShape chunk_shape(uint32_t dk, uint32_t dv) {
+    if (dk > 128) return {256, 64, 32};
+    return {dk <= 64 ? 64u : 128u, dv <= 64 ? 64u : 128u, 64};
+}
+
+// Memory for a call's states between blocks: the stream's workspace, or what the caller of run() sets aside.
+struct Room {
+    bool given = false;
+    float* floats = nullptr;
+    uint64_t count = 0;
+};
+
+// How a scan is cut: as many blocks as fill the chip, of two chunks at least; fewer where `most` floats do not hold their states.
+// *need: the floats that these blocks want.
+Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need) {
+    const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs;
+    const uint64_t spans = a.offsets != nullptr ? 1 : a.sequences;
+    // (per block and unit a state, per block and head what is kept)
+    const uint64_t each = units * shape.rows * shape.cols + a.heads;
+    Blocks b = {};
+    b.span = a.offsets != nullptr ? a.total : a.tokens;
+    uint64_t per_span = div_up(kFill, units * spans);
+    if (per_span > div_up(b.span, 2 * shape.chunk)) per_span = div_up(b.span, 2 * shape.chunk);
+    if (per_span > 1 && per_span * spans > most / each + 1) {
+        per_span = (most / each + 1) / spans;
+        if (per_span == 0) per_span = 1;
+    }
+    b.length = div_up(div_up(b.span, per_span), shape.chunk) * shape.chunk;
+    b.per_span = (uint32_t)div_up(b.span, b.length);
+    b.count = (uint32_t)(b.per_span * spans);
+    *need = b.per_span > 1 ? (b.count - 1) * each : 0;
+    return b;
+}
+
+template <typename T, typename OUT, int DK, int NT, int C>
+tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
+    const ChunkShape shape = {DK, 64 * NT, C};
+    Room room = given;
+    uint64_t need = 0;
+    Blocks b = cut(a, shape, given.given ? given.count : ~0ull, &need);
+    if (need != 0 && !given.given) {
+        const tcr_status st = partials_for(stream, need, &room.floats, &room.count);
+        if (st != TCR_OK) return st;
+        if (room.count < need) b = cut(a, shape, room.count, &need);
+    }
+    const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs, state_size = (uint64_t)DK * 64 * NT;
+    if (need != 0) {
+        b.states = room.floats;
+        b.keep = room.floats + (b.count - 1) * units * state_size;
+        attention_chunk_kernel<T, T, DK, NT, C, true><<<dim3((unsigned)((b.count - 1) * units)), dim3(kChunkThreads), 0, stream>>>(a, b);
+        if (launched("attention_chunk_kernel<states>") != TCR_OK) return TCR_ERR_HIP;
+        attention_carry_kernel<<<dim3((unsigned)(units * state_size / 1024)), dim3(256), 0, stream>>>(b, (uint32_t)slabs, state_size);
+        if (launched("attention_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
+    }
+    attention_chunk_kernel<T, OUT, DK, NT, C, false><<<dim3((unsigned)(b.count * units)), dim3(kChunkThreads), 0, stream>>>(a, b);
+    return launched("attention_chunk_kernel");
+}
+
+// Whether chunks take a scan, or it goes token by token.  (Packed sequences by their mean: one of many tokens among very many
+// without any would have a chunk's workgroups wait for the walk over them.)
+bool by_chunks(const Scan& a) {
+    if (a.total <= (a.offsets != nullptr ? 2 : kStepTokens) * a.sequences) return false;
+    for (const View* v : {&a.a, &a.b, &a.c})
+        if (v->tok < 0 || v->tok > (1 << 23)) return false;        // offsets inside a chunk are 32 bits and count upwards
+    return true;
+}
+
+template <typename T, typename OUT>
+tcr_status run(const Scan& a, const Room& room, hipStream_t stream) {
+    if (a.offsets != nullptr && a.total != 0) {
+        attention_outside_kernel<OUT><<<dim3((unsigned)div_up(a.total, 64)), dim3(256), 0, stream>>>(a);
+        if (launched("attention_outside_kernel") != TCR_OK) return TCR_ERR_HIP;
+    }
+    if (a.sequences == 0) return TCR_OK;
+    if (!by_chunks(a)) return run_steps<T, OUT>(a, stream);
+    if (a.offsets != nullptr && a.fin != nullptr) {
+        attention_empty_kernel<<<dim3((unsigned)(a.sequences * a.heads)), dim3(256), 0, stream>>>(a);
+        if (launched("attention_empty_kernel") != TCR_OK) return TCR_ERR_HIP;
+    }
+    const ChunkShape shape = chunk_shape(a.dk, a.dv);
+    if (shape.rows == 256) return run_chunks<T, OUT, 256, 1, 32>(a, room, stream);
+    if (shape.rows == 128) return shape.cols == 64 ? run_chunks<T, OUT, 128, 1, 64>(a, room, stream) : run_chunks<T, OUT, 128, 2, 64>(a, room, stream);
+    return shape.cols == 64 ? run_chunks<T, OUT, 64, 1, 64>(a, room, stream) : run_chunks<T, OUT, 64, 2, 64>(a, room, stream);
+}
+
 // Out of the type of the inputs, or binary32 (`wide`).
-tcr_status run(const Scan& a, uint32_t dtype, bool wide, hipStream_t stream) {
-    if (dtype == TCR_F16) return wide ? run<_Float16, float>(a, stream) : run<_Float16, _Float16>(a, stream);
-    return wide ? run<__bf16, float>(a, stream) : run<__bf16, __bf16>(a, stream);
+tcr_status run(const Scan& a, uint32_t dtype, bool wide, hipStream_t stream, const Room& room = Room()) {
+    if (dtype == TCR_F16) return wide ? run<_Float16, float>(a, room, stream) : run<_Float16, _Float16>(a, room, stream);
+    return wide ? run<__bf16, float>(a, room, stream) : run<__bf16, __bf16>(a, room, stream);
 }
 
 tcr_status check_states(const void* a, const void* b) { return on_boundary(a, 16) && on_boundary(b, 16) ? TCR_OK : TCR_ERR_INVALID_ARG; }
@@ -122,40 +210,53 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
     st = run(s, a.dtype, false, stream);
     if (st != TCR_OK) return st;
 
-    // dk and dv, from the last token to the first; of shared heads by way of each head's own in binary32
-    float* part = nullptr;
-    if (group > 1) {
-        const uint64_t want = (packed ? a.tokens : a.sequences * a.tokens) * a.heads * (a.dk > a.dv ? a.dk : a.dv);
-        uint64_t got = 0;
-        st = partials_for(stream, want, &part, &got);
-        if (st != TCR_OK) return st;
-        if (got < want) return TCR_ERR_WORKSPACE;
-    }
-    auto pass = [&](const View& va, const View& vb, const View& vc, uint32_t rows, uint32_t cols, void* out, bool first) {
+    // dk and dv, from the last token to the first
+    auto reversed = [&](const View& va, const View& vb, const View& vc, uint32_t rows, uint32_t cols, void* out) {
         contiguous(stride, cols);
-        Scan r = scan_of(a, va, vb, vc, group > 1 ? part : out, stride, rows, cols);
+        Scan r = scan_of(a, va, vb, vc, out, stride, rows, cols);
         r.reverse = r.late = 1;
         r.init = dfinal;
         r.init_mul = 1.0f / a.scale;
         r.fin_mul = a.scale;
-        if (first) {                     // R transposed: dv x dk
-            r.st_row = 1;
-            r.st_col = a.dv;
-        } else {
-            r.fin = dstate;
-        }
-        const tcr_status done = run(r, a.dtype, group > 1, stream);
-        if (done != TCR_OK || group == 1) return done;
-        const uint64_t count = r.total * a.kv_heads * cols;
-        if (count == 0) return TCR_OK;
-        const dim3 grid((unsigned)div_up(count, 256));
-        if (a.dtype == TCR_F16) attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(part, static_cast<_Float16*>(out), count, cols, group);
-        else attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(part, static_cast<__bf16*>(out), count, cols, group);
-        return launched("attention_shared_kernel");
+        return r;
     };
-    st = pass(vv, vo, vq, a.dv, a.dk, dk, true);
+    Scan of_k = reversed(vv, vo, vq, a.dv, a.dk, dk), of_v = reversed(vk, vq, vo, a.dk, a.dv, dv);
+    of_k.st_row = 1;                     // R transposed: dv x dk
+    of_k.st_col = a.dv;
+    of_v.fin = dstate;
+    if (group == 1) {
+        st = run(of_k, a.dtype, false, stream);
+        return st == TCR_OK ? run(of_v, a.dtype, false, stream) : st;
+    }
+    // shared ones by way of each head's own in binary32, in front of the states in the workspace
+    const uint64_t part = div_up(of_k.total * a.heads * (a.dk > a.dv ? a.dk : a.dv), 64) * 64;
+    uint64_t states = 0, got = 0;
+    for (const Scan* r : {&of_k, &of_v}) {
+        uint64_t need = 0;
+        if (by_chunks(*r)) (void)cut(*r, chunk_shape(r->dk, r->dv), ~0ull, &need);
+        if (need > states) states = need;
+    }
+    float* floats = nullptr;
+    st = partials_for(stream, part + states, &floats, &got);
     if (st != TCR_OK) return st;
-    return pass(vk, vq, vo, a.dk, a.dv, dv, false);
+    if (got < part) return TCR_ERR_WORKSPACE;
+    Room room;
+    room.given = true;
+    room.floats = floats + part;
+    room.count = got - part;
+    for (Scan* r : {&of_k, &of_v}) {
+        void* const out = r->out;
+        r->out = floats;
+        st = run(*r, a.dtype, true, stream, room);
+        if (st != TCR_OK) return st;
+        const uint64_t count = r->total * a.kv_heads * r->dv;
+        if (count == 0) continue;
+        const dim3 grid((unsigned)div_up(count, 256));
+        if (a.dtype == TCR_F16) attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(floats, static_cast<_Float16*>(out), count, r->dv, group);
+        else attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(floats, static_cast<__bf16*>(out), count, r->dv, group);
+        if (launched("attention_shared_kernel") != TCR_OK) return TCR_ERR_HIP;
+    }
+    return TCR_OK;
 }
 
 // No exception leaves the library.
