@@ -60,7 +60,12 @@ constexpr uint64_t kFill = 512;                    // workgroups that fill the c
 
 template <typename T, typename OUT>
 tcr_status run_steps(const Scan& a, hipStream_t stream) {
+    if (a.offsets != nullptr && a.total != 0) {
+        attention_outside_kernel<OUT><<<dim3((unsigned)div_up(a.total, 64)), dim3(256), 0, stream>>>(a);
+        if (launched("attention_outside_kernel") != TCR_OK) return TCR_ERR_HIP;
+    }
     const uint64_t pairs = a.sequences * a.heads;
+    if (pairs == 0) return TCR_OK;
     if (pairs * div_up(a.dv, 64) >= 1024)
         attention_step_kernel<T, 16, OUT><<<dim3((unsigned)(pairs * div_up(a.dv, 64))), dim3(kStepThreads), 0, stream>>>(a);
     else
@@ -92,15 +97,16 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
     // (per block and unit a state, per block and head what is kept)
     const uint64_t each = units * shape.rows * shape.cols + a.heads;
     Blocks b = {};
-    b.span = a.offsets != nullptr ? a.total : a.tokens;
+    const uint64_t span = a.offsets != nullptr ? a.total : a.tokens;
     uint64_t per_span = div_up(kFill, units * spans);
-    if (per_span > div_up(b.span, 2 * shape.chunk)) per_span = div_up(b.span, 2 * shape.chunk);
+    if (per_span > div_up(span, 2 * shape.chunk)) per_span = div_up(span, 2 * shape.chunk);
     if (per_span > 1 && per_span * spans > most / each + 1) {
         per_span = (most / each + 1) / spans;
         if (per_span == 0) per_span = 1;
     }
-    b.length = div_up(div_up(b.span, per_span), shape.chunk) * shape.chunk;
-    b.per_span = (uint32_t)div_up(b.span, b.length);
+    b.span = (uint32_t)span;
+    b.length = (uint32_t)(div_up(div_up(span, per_span), shape.chunk) * shape.chunk);
+    b.per_span = (uint32_t)div_up(span, b.length);
     b.count = (uint32_t)(b.per_span * spans);
     *need = b.per_span > 1 ? (b.count - 1) * each : 0;
     return b;
@@ -133,24 +139,15 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
 // Whether chunks take a scan, or it goes token by token.  (Packed sequences by their mean: one of many tokens among very many
 // without any would have a chunk's workgroups wait for the walk over them.)
 bool by_chunks(const Scan& a) {
-    if (a.total <= (a.offsets != nullptr ? 2 : kStepTokens) * a.sequences) return false;
+    if (a.sequences == 0 || a.total <= (a.offsets != nullptr ? 2 : kStepTokens) * a.sequences) return false;
     for (const View* v : {&a.a, &a.b, &a.c})
-        if (v->tok < 0 || v->tok > (1 << 23)) return false;        // offsets inside a chunk are 32 bits and count upwards
-    return true;
+        if (v->tok < 0 || v->tok > (1 << 23)) return false;        // offsets inside a chunk are 31 bits and count upwards
+    return a.out_tok >= 0 && a.out_tok <= (1 << 22);
 }
 
 template <typename T, typename OUT>
 tcr_status run(const Scan& a, const Room& room, hipStream_t stream) {
-    if (a.offsets != nullptr && a.total != 0) {
-        attention_outside_kernel<OUT><<<dim3((unsigned)div_up(a.total, 64)), dim3(256), 0, stream>>>(a);
-        if (launched("attention_outside_kernel") != TCR_OK) return TCR_ERR_HIP;
-    }
-    if (a.sequences == 0) return TCR_OK;
     if (!by_chunks(a)) return run_steps<T, OUT>(a, stream);
-    if (a.offsets != nullptr && a.fin != nullptr) {
-        attention_empty_kernel<<<dim3((unsigned)(a.sequences * a.heads)), dim3(256), 0, stream>>>(a);
-        if (launched("attention_empty_kernel") != TCR_OK) return TCR_ERR_HIP;
-    }
     const ChunkShape shape = chunk_shape(a.dk, a.dv);
     if (shape.rows == 256) return run_chunks<T, OUT, 256, 1, 32>(a, room, stream);
     if (shape.rows == 128) return shape.cols == 64 ? run_chunks<T, OUT, 128, 1, 64>(a, room, stream) : run_chunks<T, OUT, 128, 2, 64>(a, room, stream);

@@ -31,65 +31,76 @@ constexpr int kChunkThreads = 256, kChunkWaves = 4;
 
 // How the tokens are cut: spans (sequences, or all packed tokens) into blocks of `length` tokens, counted in the order of the scan.
 struct Blocks {
-    uint64_t span, length;
-    uint32_t per_span, count;
+    uint32_t span, length, per_span, count;
     float* states;              // [heads][slabs][count - 1] of what a workgroup holds: the state behind each block but the last
     float* keep;                // [heads][count - 1]: what is left behind a block of a state in front of it
 };
 
 // A chunk: tokens of sequence s at rows low .. low + len - 1 of the views.
 struct Chunk {
-    uint64_t s;
-    int64_t low;
+    uint32_t s, low;
     int len;
     bool begin, last;           // holds the first / last token of its sequence, in the order of the scan
 };
 
-struct Walk {
-    uint64_t pos, end;          // in the order of the scan
-    uint64_t s, lo, hi;         // the sequence at hand and its tokens in that order
+// (What is the same for a whole wavefront is kept in scalar registers, which the compiler has to be told of loaded values.)
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+template <typename P>
+__device__ __forceinline__ P* uniform(P* p) {
+    const uint64_t x = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<P*>((uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x));
+}
 
-    __device__ __forceinline__ bool find(const Scan& a) {
-        const uint64_t token = a.reverse ? a.total - 1 - pos : pos;
-        uint64_t from, to;
-        if (a.offsets == nullptr) {
-            s = token / a.tokens;
-            from = s * a.tokens;
-            to = from + a.tokens;
+// The chunks of a block, one after the other.
+struct Walk {
+    const uint64_t* offsets;
+    uint32_t sequences, tokens, total, reverse;
+    uint32_t pos, end;          // in the order of the scan
+    uint32_t s, lo, hi;         // the sequence at hand and its tokens in that order
+
+    __device__ __forceinline__ uint32_t cut(uint32_t i) const {
+        const uint64_t o = offsets[i];
+        return uniform(o < total ? (uint32_t)o : total);
+    }
+    // The sequence of the token at pos; false: it lies in none.
+    __device__ __forceinline__ bool find() {
+        const uint32_t token = reverse ? total - 1 - pos : pos;
+        uint32_t from, to;
+        if (offsets == nullptr) {
+            s = token / tokens;
+            from = s * tokens;
+            to = from + tokens;
         } else {
-            uint64_t low = 0, high = a.sequences;             // the last sequence that starts at or in front of the token
+            uint32_t low = 0, high = sequences;               // the last sequence that starts at or in front of the token
             while (high - low > 1) {
-                const uint64_t mid = (low + high) / 2;
-                if (a.offsets[mid] <= token) low = mid;
+                const uint32_t mid = (low + high) / 2;
+                if (cut(mid) <= token) low = mid;
                 else high = mid;
             }
             s = low;
-            from = a.offsets[s];
-            to = a.offsets[s + 1];
-            to = to < a.total ? to : a.total;
+            from = cut(s);
+            to = cut(s + 1);
             if (from > token || to <= token) return false;
         }
-        lo = a.reverse ? a.total - to : from;
-        hi = a.reverse ? a.total - from : to;
+        lo = reverse ? total - to : from;
+        hi = reverse ? total - from : to;
         return true;
     }
     template <int C>
-    __device__ __forceinline__ bool next(const Scan& a, Chunk& c) {
+    __device__ __forceinline__ bool next(Chunk& c) {
         while (pos < end) {
-            if (pos >= hi && !find(a)) {                       // (a token of no sequence)
+            if (pos >= hi && !find()) {
                 ++pos;
                 hi = pos;
                 continue;
             }
-            uint64_t stop = pos + C;
+            uint32_t stop = end - pos < C ? end : pos + C;
             stop = stop < hi ? stop : hi;
-            stop = stop < end ? stop : end;
             c.s = s;
             c.len = (int)(stop - pos);
             c.begin = pos == lo;
             c.last = stop == hi;
-            const uint64_t first = a.reverse ? a.total - stop : pos;
-            c.low = (int64_t)(a.offsets == nullptr ? first - s * a.tokens : first);
+            c.low = (reverse ? total - stop : pos) - (offsets == nullptr ? s * tokens : 0);
             pos = stop;
             return true;
         }
@@ -148,6 +159,12 @@ struct ChunkLdsOut : ChunkLds<T, DK, NT, C> {
     float p_factor[C / 16];
 };
 
+// A range of memory of whose 2^31 bytes what lies outside reads as 0 and is not written (kOutside).
+constexpr uint32_t kOutside = 0xfffffff0u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(uniform(p)), 0, 0x7fffffff, 0x00020000);
+}
+
 template <typename T, typename OUT, int DK, int NT, int C, bool STATES>
 __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const Scan a, const Blocks blocks) {
     typedef typename Bits<T>::v8 v8;
@@ -157,28 +174,36 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
     constexpr int SA = Lds::kStrideA, SB = Lds::kStrideB, SC = Lds::kStrideC, SP = Lds::kStrideP;
     __shared__ __align__(16) Lds lds;
 
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, w = (int)uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const uint32_t slabs = (a.dv + kSlab - 1) / kSlab;
     const uint32_t slab = blockIdx.x % slabs, h = blockIdx.x / slabs % a.heads, block = blockIdx.x / slabs / a.heads;
     const float log_decay = decay_of(a, h);
     constexpr int kHeld = KT * NT * 4;                              // floats of S a lane holds
-    const int64_t state_size = (int64_t)kChunkThreads * kHeld;
+    constexpr uint32_t kStateSize = kChunkThreads * kHeld;
+    // a head's rows, and its states
+    const T* const pa = static_cast<const T*>(a.a.p) + (int64_t)(h / a.a.group) * a.a.head;
+    const T* const pb = static_cast<const T*>(a.b.p) + (int64_t)(h / a.b.group) * a.b.head;
+    const T* const pc = static_cast<const T*>(a.c.p) + (int64_t)(h / a.c.group) * a.c.head + slab * kSlab;
+    OUT* const po = static_cast<OUT*>(a.out) + (int64_t)h * a.out_head + slab * kSlab;
+    const uint32_t state_floats = a.dk * a.dv, left = a.dv - slab * kSlab;        // (columns of c from this slab's first on)
 
     // the block's tokens, in the order of the scan
     Walk walk;
-    walk.pos = block / blocks.per_span * blocks.span + block % blocks.per_span * blocks.length;
-    {
-        const uint64_t span_end = (block / blocks.per_span + 1) * blocks.span;
-        walk.end = walk.pos + blocks.length;
-        walk.end = walk.end < span_end ? walk.end : span_end;
-        walk.s = walk.lo = walk.hi = 0;
-    }
-    const uint64_t block_start = walk.pos;
+    walk.offsets = a.offsets;
+    walk.sequences = (uint32_t)a.sequences;
+    walk.tokens = (uint32_t)a.tokens;
+    walk.total = (uint32_t)a.total;
+    walk.reverse = a.reverse;
+    const uint32_t span_first = block / blocks.per_span * blocks.span, in_span = block % blocks.per_span * blocks.length;
+    const uint32_t block_start = span_first + in_span;
+    walk.pos = block_start;
+    walk.end = blocks.span - in_span < blocks.length ? span_first + blocks.span : block_start + blocks.length;
+    walk.s = walk.lo = walk.hi = 0;
     if constexpr (STATES) {
         // only the sequence that goes on behind the block counts
         walk.pos = walk.end - 1;
-        const bool some = walk.find(a);
-        const uint64_t from = some && walk.lo > block_start ? walk.lo : block_start;
+        const bool some = walk.find();
+        const uint32_t from = some && walk.lo > block_start ? walk.lo : block_start;
         if (slab == 0 && threadIdx.x == 0)
             blocks.keep[(uint64_t)h * (blocks.count - 1) + block] =
                 some && walk.lo < block_start ? decayed(log_decay, (float)(walk.end - block_start)) : 0.0f;
@@ -192,40 +217,78 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
     constexpr int kPasses = C / kPassRows, kPassesC = C / kPassRowsC;
     u4v ra[kPasses], rb[kPasses], rc[kPassesC];
     const int row = threadIdx.x / kVecs, col = threadIdx.x % kVecs * 8, row_c = threadIdx.x / kCVecs, col_c = threadIdx.x % kCVecs * 8;
-    auto fetch = [&](const View& v, const Chunk& c, int r0, uint32_t column, bool inside, int step, u4v* to, auto passes) {
-        const T* base = static_cast<const T*>(v.p) + (int64_t)(a.offsets == nullptr ? c.s : 0) * v.seq + c.low * v.tok + (int64_t)(h / v.group) * v.head;
-        __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, 0x7fffffff, 0x00020000);
-        const uint32_t pitch = (uint32_t)v.tok * sizeof(T);
+    const int forwards = a.reverse ? -1 : 1;
+    auto fetch = [&](const T* head, const View& v, const Chunk& c, int r0, bool inside, uint32_t column, int step, u4v* to, auto passes) {
+        const uint32_t tok = (uint32_t)v.tok;
+        const __amdgpu_buffer_rsrc_t buffer = buffer_at(head + ((a.offsets == nullptr ? (int64_t)c.s * v.seq : 0) + (int64_t)c.low * tok));
+        const int rows = inside ? c.len : 0, first = a.reverse ? c.len - 1 : 0;
 #pragma unroll
         for (int p = 0; p < decltype(passes)::value; ++p) {
             const int r = r0 + p * step;
-            const uint32_t at = (uint32_t)(a.reverse ? c.len - 1 - r : r) * pitch + column * (uint32_t)sizeof(T);
-            to[p] = __builtin_amdgcn_raw_buffer_load_b128(buffer, inside && r < c.len ? at : 0xfffffff0u, 0, 0);
+            const uint32_t at = ((uint32_t)(first + forwards * r) * tok + column) * (uint32_t)sizeof(T);
+            to[p] = __builtin_amdgcn_raw_buffer_load_b128(buffer, r < rows ? at : kOutside, 0, 0);
         }
     };
     auto fetch_all = [&](const Chunk& c) {
-        if constexpr (!STATES) fetch(a.a, c, row, col, (uint32_t)col < a.dk, kPassRows, ra, std::integral_constant<int, kPasses>());
-        fetch(a.b, c, row, col, (uint32_t)col < a.dk, kPassRows, rb, std::integral_constant<int, kPasses>());
-        fetch(a.c, c, row_c, slab * kSlab + col_c, slab * kSlab + col_c < a.dv, kPassRowsC, rc, std::integral_constant<int, kPassesC>());
+        if constexpr (!STATES) fetch(pa, a.a, c, row, (uint32_t)col < a.dk, col, kPassRows, ra, std::integral_constant<int, kPasses>());
+        fetch(pb, a.b, c, row, (uint32_t)col < a.dk, col, kPassRows, rb, std::integral_constant<int, kPasses>());
+        fetch(pc, a.c, c, row_c, (uint32_t)col_c < left, col_c, kPassRowsC, rc, std::integral_constant<int, kPassesC>());
     };
 
+    // S: rows 16 mt + 4 g + r, columns 16 (NT w + nt) + n of the slab
     f4v S[KT][NT];
-    const uint32_t dv0 = slab * kSlab + w * 16 * NT + n;             // this lane's columns of S: dv0 + 16 nt; rows: 16 mt + 4 g + r
-    auto from_states = [&](const float* from) {
-#pragma unroll
-        for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[mt][nt] = *reinterpret_cast<const f4v*>(from + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
-    };
     auto clear = [&] {
 #pragma unroll
         for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) S[mt][nt] = f4v{0, 0, 0, 0};
     };
-    float* const own_states = blocks.states + ((int64_t)(h * slabs + slab) * (blocks.count - 1) + block) * state_size;
+    // element of S = f(element, byte offset in a state) for all of them; the offsets are worked out where they are used, which is rare
+    auto each = [&](auto f) {
+        uint32_t k0 = 4 * g, v0 = w * 16 * NT + n;
+        asm volatile("" : "+v"(k0), "+v"(v0));
+        const uint32_t st_row = (uint32_t)a.st_row, st_col = (uint32_t)a.st_col;
+#pragma unroll
+        for (int mt = 0; mt < KT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t k = k0 + mt * 16 + r, v = v0 + 16 * nt;
+                    S[mt][nt][r] = f(S[mt][nt][r], k < a.dk && v < left ? (k * st_row + (v + slab * kSlab) * st_col) * 4 : kOutside);
+                }
+    };
+    float* const own_states = blocks.states + ((int64_t)(h * slabs + slab) * (blocks.count - 1) + block) * kStateSize;
     clear();
-    if (!STATES && block % blocks.per_span != 0) from_states(own_states - state_size);       // (0 where a sequence starts with the block)
+    if (!STATES && block % blocks.per_span != 0) {                  // (not looked at where a sequence starts with the block)
+        const float* from = own_states - kStateSize;
+#pragma unroll
+        for (int mt = 0; mt < KT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[mt][nt] = *reinterpret_cast<const f4v*>(from + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
+    }
+
+    if (!STATES && a.offsets != nullptr) {
+        // zeros in the rows of the block's tokens that lie in no sequence
+        const uint32_t from = a.reverse ? walk.total - walk.end : block_start, to = a.reverse ? walk.total - block_start : walk.end;
+        const uint32_t first = walk.cut(0), last = walk.cut(walk.sequences);
+        auto zeros = [&](uint32_t t, uint32_t end) {
+            for (t += threadIdx.x / kSlab; t < end; t += kChunkThreads / kSlab)
+                if (threadIdx.x % kSlab < left) po[(int64_t)t * a.out_tok + threadIdx.x % kSlab] = (OUT)0.0f;
+        };
+        zeros(from, to < first ? to : first);
+        zeros(from > last ? from : last, to);
+        // final states of sequences without tokens: the first ones
+        if (block == 0 && slab == 0 && a.fin != nullptr)
+            for (uint32_t s0 = 0; s0 < walk.sequences; s0 += 64) {
+                uint64_t empty = __ballot(s0 + lane < walk.sequences && span_of(a, s0 + lane).count == 0);
+                for (; empty != 0; empty &= empty - 1) {
+                    const int64_t at = ((int64_t)(s0 + __builtin_ctzll(empty)) * a.heads + h) * state_floats;
+                    for (uint32_t i = threadIdx.x * 4; i < state_floats; i += kChunkThreads * 4)
+                        *reinterpret_cast<f4v*>(a.fin + at + i) = a.init != nullptr ? *reinterpret_cast<const f4v*>(a.init + at + i) : f4v{0, 0, 0, 0};
+                }
+            }
+    }
 
     // the diagonal's decays of the scores this wavefront computes: lambda^(n - 4g - r), 0 above the diagonal
     __syncthreads();
@@ -234,7 +297,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
     for (int r = 0; r < 4; ++r) diagonal[r] = n >= 4 * g + r ? lds.powers[n - 4 * g - r < 0 ? 0 : n - 4 * g - r] : 0.0f;
 
     Chunk now, ahead;
-    bool more = walk.next<C>(a, now);
+    bool more = walk.next<C>(now);
     if (more) fetch_all(now);
     while (more) {
         // ---- the chunk's rows into LDS (all reads of the last chunk's are done)
@@ -246,21 +309,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
 #pragma unroll
         for (int p = 0; p < kPassesC; ++p) *reinterpret_cast<u4v*>(&lds.c[(row_c + p * kPassRowsC) * SC + col_c]) = rc[p];
         __syncthreads();
-        more = walk.next<C>(a, ahead);
+        more = walk.next<C>(ahead);
         if (more) fetch_all(ahead);
 
         if (now.begin) {
             if (a.init != nullptr) {
-                const float* from = a.init + ((int64_t)now.s * a.heads + h) * a.dk * a.dv;
-#pragma unroll
-                for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const uint32_t k = mt * 16 + 4 * g + r, v = dv0 + 16 * nt;
-                            S[mt][nt][r] = k < a.dk && v < a.dv ? from[(int64_t)k * a.st_row + (int64_t)v * a.st_col] * a.init_mul : 0.0f;
-                        }
+                const __amdgpu_buffer_rsrc_t from = buffer_at(a.init + ((int64_t)now.s * a.heads + h) * state_floats);
+                each([&](float, uint32_t at) { return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, 0)) * a.init_mul; });
             } else {
                 clear();
             }
@@ -270,7 +325,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
         f4v o[CT][NT];
         if constexpr (!STATES) {
             // ---- scores: tile row `it` by wavefront it
-            for (int it = w; it < CT; it += kChunkWaves) {
+            if (w < CT) {
+                const int it = w;
                 f4v s[CT];
 #pragma unroll
                 for (int jt = 0; jt < CT; ++jt) s[jt] = f4v{0, 0, 0, 0};
@@ -385,20 +441,22 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) o[it][nt] = mfma(cols[ks][nt], scores, o[it][nt]);
                     }
-            OUT* out = static_cast<OUT*>(a.out) + (int64_t)(a.offsets == nullptr ? now.s : 0) * a.out_seq + now.low * a.out_tok + (int64_t)h * a.out_head;
+            const uint32_t tok = (uint32_t)a.out_tok;
+            const __amdgpu_buffer_rsrc_t out = buffer_at(po + ((a.offsets == nullptr ? (int64_t)now.s * a.out_seq : 0) + (int64_t)now.low * tok));
 #pragma unroll
             for (int it = 0; it < CT; ++it) {
                 const int i = it * 16 + n;
-                if (i >= now.len) continue;
                 const float f = a.out_scale * (kHalf ? reciprocal_power(lds.p_factor[it]) : 1.0f);
-                OUT* to = out + (int64_t)(a.reverse ? now.len - 1 - i : i) * a.out_tok;
+                const uint32_t to = (uint32_t)(a.reverse ? now.len - 1 - i : i) * tok;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const uint32_t v = slab * kSlab + (w * NT + nt) * 16 + 4 * g;
-                    if (v >= a.dv) continue;
-                    typedef OUT o4 __attribute__((ext_vector_type(4), aligned(sizeof(OUT))));
+                    const uint32_t v = (w * NT + nt) * 16 + 4 * g;
+                    const uint32_t at = i < now.len && v < left ? (to + v) * (uint32_t)sizeof(OUT) : kOutside;
+                    typedef OUT o4 __attribute__((ext_vector_type(4)));
                     const f4v x = o[it][nt] * f;
-                    *reinterpret_cast<o4*>(to + v) = o4{(OUT)x[0], (OUT)x[1], (OUT)x[2], (OUT)x[3]};
+                    const o4 y = {(OUT)x[0], (OUT)x[1], (OUT)x[2], (OUT)x[3]};
+                    if constexpr (sizeof(OUT) == 2) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2v, y), out, at, 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, y), out, at, 0, 0);
                 }
             }
         }
@@ -454,17 +512,12 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
                 for (int nt = 0; nt < NT; ++nt) S[mt][nt] *= f;
         }
         if (!STATES && now.last && a.fin != nullptr) {
-            float* to = a.fin + ((int64_t)now.s * a.heads + h) * a.dk * a.dv;
+            const __amdgpu_buffer_rsrc_t to = buffer_at(a.fin + ((int64_t)now.s * a.heads + h) * state_floats);
             const float mul = a.late ? lds.powers[1] * a.fin_mul : a.fin_mul;
-#pragma unroll
-            for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const uint32_t k = mt * 16 + 4 * g + r, v = dv0 + 16 * nt;
-                        if (k < a.dk && v < a.dv) to[(int64_t)k * a.st_row + (int64_t)v * a.st_col] = S[mt][nt][r] * mul;
-                    }
+            each([&](float x, uint32_t at) {
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x * mul), to, at, 0, 0);
+                return x;
+            });
         }
         __syncthreads();                                                           // all reads of this chunk's rows are done
         now = ahead;
@@ -483,19 +536,20 @@ __global__ __launch_bounds__(256) void attention_carry_kernel(const Blocks block
     f4v* states = reinterpret_cast<f4v*>(blocks.states + group * (blocks.count - 1) * state_size + at % state_size);
     const float* keep = blocks.keep + group / slabs * (blocks.count - 1);
     f4v carry = {0, 0, 0, 0};
-#pragma unroll 4
-    for (uint32_t n = 0; n + 1 < blocks.count; ++n) {
-        carry = states[n * (state_size / 4)] + carry * keep[n];
-        states[n * (state_size / 4)] = carry;
+    // (the loads of many blocks at once, then their sums)
+    constexpr uint32_t kAtOnce = 16;
+    for (uint32_t n0 = 0; n0 + 1 < blocks.count; n0 += kAtOnce) {
+        f4v own[kAtOnce];
+        const uint32_t end = blocks.count - 1;
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) own[i] = states[(n0 + i < end ? n0 + i : end - 1) * (state_size / 4)];
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i)
+            if (n0 + i < end) {
+                carry = own[i] + carry * keep[n0 + i];
+                states[(n0 + i) * (state_size / 4)] = carry;
+            }
     }
-}
-
-// Final states of sequences without tokens: the first ones.
-__global__ __launch_bounds__(256) void attention_empty_kernel(const Scan a) {
-    const uint64_t s = blockIdx.x / a.heads;
-    if (span_of(a, s).count != 0) return;
-    const uint64_t size = (uint64_t)a.dk * a.dv, from = (uint64_t)blockIdx.x * size;
-    for (uint64_t i = threadIdx.x; i < size; i += 256) a.fin[from + i] = a.init != nullptr ? a.init[from + i] : 0.0f;
 }
 
 }  // namespace layers
