@@ -112,9 +112,9 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
     return b;
 }
 
-template <typename T, typename OUT, int DK, int NT, int C>
+template <typename T, typename OUT, int DK, int W, int NT, int C>
 tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
-    const ChunkShape shape = {DK, 64 * NT, C};
+    const ChunkShape shape = {DK, 16 * W * NT, C};
     Room room = given;
     uint64_t need = 0;
     Blocks b = cut(a, shape, given.given ? given.count : ~0ull, &need);
@@ -123,16 +123,16 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
         if (st != TCR_OK) return st;
         if (room.count < need) b = cut(a, shape, room.count, &need);
     }
-    const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs, state_size = (uint64_t)DK * 64 * NT;
+    const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs, state_size = (uint64_t)DK * shape.cols;
     if (need != 0) {
         b.states = room.floats;
         b.keep = room.floats + (b.count - 1) * units * state_size;
-        attention_chunk_kernel<T, T, DK, NT, C, true><<<dim3((unsigned)((b.count - 1) * units)), dim3(kChunkThreads), 0, stream>>>(a, b);
+        attention_chunk_kernel<T, T, DK, W, NT, C, true><<<dim3((unsigned)((b.count - 1) * units)), dim3(64 * W), 0, stream>>>(a, b);
         if (launched("attention_chunk_kernel<states>") != TCR_OK) return TCR_ERR_HIP;
         attention_carry_kernel<<<dim3((unsigned)(units * state_size / 1024)), dim3(256), 0, stream>>>(b, (uint32_t)slabs, state_size);
         if (launched("attention_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
     }
-    attention_chunk_kernel<T, OUT, DK, NT, C, false><<<dim3((unsigned)(b.count * units)), dim3(kChunkThreads), 0, stream>>>(a, b);
+    attention_chunk_kernel<T, OUT, DK, W, NT, C, false><<<dim3((unsigned)(b.count * units)), dim3(64 * W), 0, stream>>>(a, b);
     return launched("attention_chunk_kernel");
 }
 
@@ -149,9 +149,9 @@ template <typename T, typename OUT>
 tcr_status run(const Scan& a, const Room& room, hipStream_t stream) {
     if (!by_chunks(a)) return run_steps<T, OUT>(a, stream);
     const ChunkShape shape = chunk_shape(a.dk, a.dv);
-    if (shape.rows == 256) return run_chunks<T, OUT, 256, 1, 32>(a, room, stream);
-    if (shape.rows == 128) return shape.cols == 64 ? run_chunks<T, OUT, 128, 1, 64>(a, room, stream) : run_chunks<T, OUT, 128, 2, 64>(a, room, stream);
-    return shape.cols == 64 ? run_chunks<T, OUT, 64, 1, 64>(a, room, stream) : run_chunks<T, OUT, 64, 2, 64>(a, room, stream);
+    if (shape.rows == 256) return run_chunks<T, OUT, 256, 4, 1, 32>(a, room, stream);
+    if (shape.rows == 128) return shape.cols == 64 ? run_chunks<T, OUT, 128, 4, 1, 64>(a, room, stream) : run_chunks<T, OUT, 128, 8, 1, 64>(a, room, stream);
+    return shape.cols == 64 ? run_chunks<T, OUT, 64, 4, 1, 64>(a, room, stream) : run_chunks<T, OUT, 64, 8, 1, 64>(a, room, stream);
 }
 
 // Out of the type of the inputs, or binary32 (`wide`).

@@ -4,7 +4,7 @@
 // i.e. a product with a triangular matrix inside the chunk and a carry between chunks: the scan of tiles that the library's scans
 // are, with a matrix for the running sum.
 //
-// One workgroup of 4 wavefronts takes a block of consecutive tokens of one head, chunk after chunk, and a slab of 64 * NT columns
+// One workgroup of W wavefronts takes a block of consecutive tokens of one head, chunk after chunk, and a slab of 16 * W * NT columns
 // of c; each wavefront holds its 16 * NT columns of S in accumulator registers all along.  The chunk's rows pass through
 // LDS once; the next chunk's are loaded into registers meanwhile.  Where sequences and heads are too few to fill the chip, tokens are cut into
 // several blocks: a first kernel (STATES) leaves the state that each block alone arrives at, a second adds up what
@@ -26,8 +26,6 @@
 
 namespace tcr {
 namespace layers {
-
-constexpr int kChunkThreads = 256, kChunkWaves = 4;
 
 // How the tokens are cut: spans (sequences, or all packed tokens) into blocks of `length` tokens, counted in the order of the scan.
 struct Blocks {
@@ -130,6 +128,36 @@ __device__ __forceinline__ float settled(float x) {
     asm("" : "+v"(x));
     return x;
 }
+// Two numbers as PARTS pairs of 16-bit ones whose sums they are.  binary16: every part but the last is cut off, not rounded (one instruction for
+// the pair; what is cut off is the next part's), the last one rounded if `fine`.
+template <typename T, int PARTS>
+__device__ __forceinline__ void split(float a, float b, uint32_t (&parts)[PARTS], bool fine) {
+    if constexpr (std::is_same<T, _Float16>::value) {
+        a = settled(a);
+        b = settled(b);
+    }
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+        if constexpr (std::is_same<T, _Float16>::value) {
+            typedef __fp16 cut2 __attribute__((ext_vector_type(2)));
+            typedef _Float16 pair __attribute__((ext_vector_type(2)));
+            if (p + 1 < PARTS || !fine) {
+                const pair h = __builtin_bit_cast(pair, (cut2)__builtin_amdgcn_cvt_pkrtz(a, b));
+                parts[p] = __builtin_bit_cast(uint32_t, h);
+                a -= (float)h[0];
+                b -= (float)h[1];
+            } else {
+                parts[p] = __builtin_bit_cast(uint32_t, pair{(_Float16)a, (_Float16)b});
+            }
+        } else {
+            typedef __bf16 pair __attribute__((ext_vector_type(2)));
+            typedef float wide __attribute__((ext_vector_type(2)));
+            parts[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector(wide{a, b}, pair));
+            a -= __builtin_bit_cast(float, parts[p] << 16);
+            b -= __builtin_bit_cast(float, parts[p] & 0xffff0000u);
+        }
+    }
+}
 __device__ __forceinline__ float wave_largest(float x) {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
@@ -144,19 +172,19 @@ __device__ __forceinline__ float near_top(float largest) {
 }
 __device__ __forceinline__ float reciprocal_power(float f) { return __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, f)); }
 
-template <typename T, int DK, int NT, int C>
+template <typename T, int DK, int COLS, int C>
 struct ChunkLds {
     // (rows 16 bytes beyond a multiple of 256: reads of 8 or 16 bytes from 16 rows meet no bank twice; 32 bytes: reads of columns)
-    static constexpr int kStrideA = DK + 8, kStrideB = DK + 16, kStrideC = 64 * NT + 16, kStrideP = C + 16;
+    static constexpr int kStrideA = DK + 8, kStrideB = DK + 16, kStrideC = COLS + 16, kStrideP = C + 16;
     alignas(16) T b[C * kStrideB];
     alignas(16) T c[C * kStrideC];
     float powers[C + 1];                     // lambda^0 .. lambda^C
 };
-template <typename T, int DK, int NT, int C>
-struct ChunkLdsOut : ChunkLds<T, DK, NT, C> {
-    alignas(16) T a[C * ChunkLds<T, DK, NT, C>::kStrideA];
-    alignas(16) T p[2][C * ChunkLds<T, DK, NT, C>::kStrideP];
-    float p_factor[C / 16];
+template <typename T, int DK, int COLS, int C>
+struct ChunkLdsOut : ChunkLds<T, DK, COLS, C> {
+    alignas(16) T a[C * ChunkLds<T, DK, COLS, C>::kStrideA];
+    alignas(16) T p[2][C * ChunkLds<T, DK, COLS, C>::kStrideP];
+    float p_factor[C / 16][C / 32];          // of the scores of 16 rows and 32 columns
 };
 
 // A range of memory of whose 2^31 bytes what lies outside reads as 0 and is not written (kOutside).
@@ -165,16 +193,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(uniform(p)), 0, 0x7fffffff, 0x00020000);
 }
 
-template <typename T, typename OUT, int DK, int NT, int C, bool STATES>
-__global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const Scan a, const Blocks blocks) {
+template <typename T, typename OUT, int DK, int W, int NT, int C, bool STATES>
+__global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Scan a, const Blocks blocks) {
     typedef typename Bits<T>::v8 v8;
     constexpr bool kHalf = std::is_same<T, _Float16>::value;
-    constexpr int CT = C / 16, KT = DK / 16, kParts = kHalf ? 2 : 3, kSlab = 64 * NT;
-    typedef typename std::conditional<STATES, ChunkLds<T, DK, NT, C>, ChunkLdsOut<T, DK, NT, C>>::type Lds;
+    constexpr int CT = C / 16, KT = DK / 16, kParts = kHalf ? 2 : 3, kSlab = 16 * W * NT, KS = C / 32;
+    constexpr int kChunkThreads = 64 * W;
+    typedef typename std::conditional<STATES, ChunkLds<T, DK, kSlab, C>, ChunkLdsOut<T, DK, kSlab, C>>::type Lds;
     constexpr int SA = Lds::kStrideA, SB = Lds::kStrideB, SC = Lds::kStrideC, SP = Lds::kStrideP;
     __shared__ __align__(16) Lds lds;
 
-    const int lane = threadIdx.x & 63, w = (int)uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int w = (int)uniform(threadIdx.x >> 6);
+    int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const uint32_t slabs = (a.dv + kSlab - 1) / kSlab;
     const uint32_t slab = blockIdx.x % slabs, h = blockIdx.x / slabs % a.heads, block = blockIdx.x / slabs / a.heads;
     const float log_decay = decay_of(a, h);
@@ -216,7 +246,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
     constexpr int kVecs = DK / 8, kCVecs = kSlab / 8, kPassRows = kChunkThreads / kVecs, kPassRowsC = kChunkThreads / kCVecs;
     constexpr int kPasses = C / kPassRows, kPassesC = C / kPassRowsC;
     u4v ra[kPasses], rb[kPasses], rc[kPassesC];
-    const int row = threadIdx.x / kVecs, col = threadIdx.x % kVecs * 8, row_c = threadIdx.x / kCVecs, col_c = threadIdx.x % kCVecs * 8;
+    int row = threadIdx.x / kVecs, col = threadIdx.x % kVecs * 8, row_c = threadIdx.x / kCVecs, col_c = threadIdx.x % kCVecs * 8;
     const int forwards = a.reverse ? -1 : 1;
     auto fetch = [&](const T* head, const View& v, const Chunk& c, int r0, bool inside, uint32_t column, int step, u4v* to, auto passes) {
         const uint32_t tok = (uint32_t)v.tok;
@@ -243,10 +273,9 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) S[mt][nt] = f4v{0, 0, 0, 0};
     };
-    // element of S = f(element, byte offset in a state) for all of them; the offsets are worked out where they are used, which is rare
+    // element of S = f(element, byte offset in a state) for all of them
     auto each = [&](auto f) {
         uint32_t k0 = 4 * g, v0 = w * 16 * NT + n;
-        asm volatile("" : "+v"(k0), "+v"(v0));
         const uint32_t st_row = (uint32_t)a.st_row, st_col = (uint32_t)a.st_col;
 #pragma unroll
         for (int mt = 0; mt < KT; ++mt)
@@ -290,16 +319,22 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
             }
     }
 
-    // the diagonal's decays of the scores this wavefront computes: lambda^(n - 4g - r), 0 above the diagonal
     __syncthreads();
-    float diagonal[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) diagonal[r] = n >= 4 * g + r ? lds.powers[n - 4 * g - r < 0 ? 0 : n - 4 * g - r] : 0.0f;
-
     Chunk now, ahead;
     bool more = walk.next<C>(now);
     if (more) fetch_all(now);
     while (more) {
+        // (addresses are worked out in every chunk: kept in registers all along they would push others to memory, and the wait for one of those
+        // is a wait for the next chunk's rows too)
+        int t = threadIdx.x;
+        asm volatile("" : "+v"(t));
+        lane = t & 63;
+        n = lane & 15;
+        g = lane >> 4;
+        row = t / kVecs;
+        col = t % kVecs * 8;
+        row_c = t / kCVecs;
+        col_c = t % kCVecs * 8;
         // ---- the chunk's rows into LDS (all reads of the last chunk's are done)
         if constexpr (!STATES)
 #pragma unroll
@@ -324,49 +359,40 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
 
         f4v o[CT][NT];
         if constexpr (!STATES) {
-            // ---- scores: tile row `it` by wavefront it
-            if (w < CT) {
-                const int it = w;
-                f4v s[CT];
-#pragma unroll
-                for (int jt = 0; jt < CT; ++jt) s[jt] = f4v{0, 0, 0, 0};
+            // ---- scores, 16 rows and 32 columns at a time, the rows by lanes
+            for (int task = w; task < CT * KS; task += W) {
+                const int it = task / KS, jp = task % KS * 2;                      // (column tiles jp and jp + 1)
+                if (jp > it) continue;
+                f4v s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
                 for (int ks = 0; ks < DK / 32; ++ks) {
                     const v8 rows = *reinterpret_cast<const v8*>(&lds.a[(it * 16 + n) * SA + ks * 32 + 8 * g]);
-#pragma unroll
-                    for (int jt = 0; jt < CT; ++jt)
-                        if (jt <= it) s[jt] = mfma(*reinterpret_cast<const v8*>(&lds.b[(jt * 16 + n) * SB + ks * 32 + 8 * g]), rows, s[jt]);
+                    s[0] = mfma(*reinterpret_cast<const v8*>(&lds.b[(jp * 16 + n) * SB + ks * 32 + 8 * g]), rows, s[0]);
+                    if (jp < it) s[1] = mfma(*reinterpret_cast<const v8*>(&lds.b[(jp * 16 + 16 + n) * SB + ks * 32 + 8 * g]), rows, s[1]);
                 }
                 float largest = 0.0f;
 #pragma unroll
-                for (int jt = 0; jt < CT; ++jt) {
-                    if (jt > it) continue;
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         // (a score above the diagonal is dropped, whatever it is)
-                        const float d = jt == it ? diagonal[r] : lds.powers[(it - jt) * 16 + n - 4 * g - r];
-                        s[jt][r] = jt == it && n < 4 * g + r ? 0.0f : s[jt][r] * d;
-                        if constexpr (kHalf) largest = fmaxf(largest, fabsf(s[jt][r]));
+                        const int steps = (it - jp - t) * 16 + n - 4 * g - r;
+                        s[t][r] = steps < 0 ? 0.0f : s[t][r] * lds.powers[steps < 0 ? 0 : steps];
+                        if constexpr (kHalf) largest = fmaxf(largest, fabsf(s[t][r]));
                     }
-                }
                 float factor = 1.0f;
                 if constexpr (kHalf) {
                     factor = near_top(wave_largest(largest));
-                    if (lane == 0) lds.p_factor[it] = factor;
+                    if (lane == 0) lds.p_factor[it][jp / 2] = factor;
                 }
 #pragma unroll
-                for (int jt = 0; jt < CT; ++jt) {
-                    if (jt > (it | 1)) continue;
-                    T hi[4], lo[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float x = kHalf ? settled(s[jt][r] * factor) : s[jt][r];
-                        hi[r] = (T)x;
-                        lo[r] = (T)(x - (float)hi[r]);
-                    }
-                    typedef T v4 __attribute__((ext_vector_type(4)));
-                    *reinterpret_cast<v4*>(&lds.p[0][(it * 16 + n) * SP + jt * 16 + 4 * g]) = v4{hi[0], hi[1], hi[2], hi[3]};
-                    *reinterpret_cast<v4*>(&lds.p[1][(it * 16 + n) * SP + jt * 16 + 4 * g]) = v4{lo[0], lo[1], lo[2], lo[3]};
+                for (int t = 0; t < 2; ++t) {
+                    uint32_t x[2], y[2];
+                    split<T, 2>(s[t][0] * factor, s[t][1] * factor, x, false);
+                    split<T, 2>(s[t][2] * factor, s[t][3] * factor, y, false);
+                    const int at = (it * 16 + n) * SP + (jp + t) * 16 + 4 * g;
+                    *reinterpret_cast<u2v*>(&lds.p[0][at]) = u2v{x[0], y[0]};
+                    *reinterpret_cast<u2v*>(&lds.p[1][at]) = u2v{x[1], y[1]};
                 }
             }
             // ---- what the state in front of the chunk gives
@@ -387,31 +413,35 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
                 for (int nt = 0; nt < NT; ++nt) o[it][nt] = f4v{0, 0, 0, 0};
 #pragma unroll
             for (int ks = 0; ks < DK / 32; ++ks) {
-                v8 hi[NT], lo[NT];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const float x = kHalf ? settled(S[2 * ks + (r >> 2)][nt][r & 3] * factor) : S[2 * ks + (r >> 2)][nt][r & 3];
-                        hi[nt][r] = (T)x;
-                        lo[nt][r] = (T)(x - (float)hi[nt][r]);
-                    }
+                v8 rows[CT];
 #pragma unroll
                 for (int it = 0; it < CT; ++it) {
                     const T* from = &lds.a[(it * 16 + n) * SA + ks * 32 + 4 * g];
-                    const v8 rows = joined<T>(*reinterpret_cast<const s4v*>(from), *reinterpret_cast<const s4v*>(from + 16));
+                    rows[it] = joined<T>(*reinterpret_cast<const s4v*>(from), *reinterpret_cast<const s4v*>(from + 16));
+                }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        o[it][nt] = mfma(hi[nt], rows, o[it][nt]);
-                        o[it][nt] = mfma(lo[nt], rows, o[it][nt]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    u4v parts[2];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const f4v x = S[2 * ks + (r >> 1)][nt];
+                        const int e = (r & 1) * 2;
+                        uint32_t y[2];
+                        split<T, 2>(kHalf ? x[e] * factor : x[e], kHalf ? x[e + 1] * factor : x[e + 1], y, false);
+                        parts[0][r] = y[0];
+                        parts[1][r] = y[1];
                     }
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int it = 0; it < CT; ++it) o[it][nt] = mfma(__builtin_bit_cast(v8, parts[p]), rows[it], o[it][nt]);
                 }
             }
             __syncthreads();                                                       // the scores are there
 #pragma unroll
             for (int it = 0; it < CT; ++it) {
                 float f = lds.powers[it * 16 + n + 1 - late];
-                if constexpr (kHalf) f *= reciprocal_power(factor) * lds.p_factor[it];
+                if constexpr (kHalf) f *= reciprocal_power(factor) * lds.p_factor[it][0];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) o[it][nt] *= f;
             }
@@ -432,21 +462,27 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
             }
         if constexpr (!STATES) {
 #pragma unroll
-            for (int ks = 0; ks < C / 32; ++ks)
+            for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int it = 2 * ks; it < CT; ++it)
+                for (int it = 2 * ks; it < CT; ++it) {
+                    if (kHalf && ks > 0) {                                         // from the factor of the columns in front to these
+                        const float f = lds.p_factor[it][ks] * reciprocal_power(lds.p_factor[it][ks - 1]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) o[it][nt] *= f;
+                    }
 #pragma unroll
                     for (int part = 0; part < 2; ++part) {
                         const v8 scores = *reinterpret_cast<const v8*>(&lds.p[part][(it * 16 + n) * SP + ks * 32 + 8 * g]);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) o[it][nt] = mfma(cols[ks][nt], scores, o[it][nt]);
                     }
+                }
             const uint32_t tok = (uint32_t)a.out_tok;
             const __amdgpu_buffer_rsrc_t out = buffer_at(po + ((a.offsets == nullptr ? (int64_t)now.s * a.out_seq : 0) + (int64_t)now.low * tok));
 #pragma unroll
             for (int it = 0; it < CT; ++it) {
                 const int i = it * 16 + n;
-                const float f = a.out_scale * (kHalf ? reciprocal_power(lds.p_factor[it]) : 1.0f);
+                const float f = a.out_scale * (kHalf ? reciprocal_power(lds.p_factor[it][it / 2]) : 1.0f);
                 const uint32_t to = (uint32_t)(a.reverse ? now.len - 1 - i : i) * tok;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -477,23 +513,22 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
         }
 #pragma unroll
         for (int ks = 0; ks < C / 32; ++ks) {
-            v8 part[kParts][NT];
+            u4v part[kParts][NT];
             float decays[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
                 const int steps = now.len - 1 - (ks * 32 + 8 * g + r);
-                decays[r] = lds.powers[steps < 0 ? 0 : steps] * factor_c;
+                decays[r] = lds.powers[steps < 0 ? 0 : steps];
+                if constexpr (kHalf) decays[r] *= factor_c;
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    float x = settled((float)cols[ks][nt][r] * decays[r]);
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t y[kParts];
+                    split<T, kParts>((float)cols[ks][nt][2 * r] * decays[2 * r], (float)cols[ks][nt][2 * r + 1] * decays[2 * r + 1], y, true);
 #pragma unroll
-                    for (int p = 0; p < kParts; ++p) {
-                        part[p][nt][r] = (T)x;
-                        x -= (float)part[p][nt][r];
-                    }
+                    for (int p = 0; p < kParts; ++p) part[p][nt][r] = y[p];
                 }
 #pragma unroll
             for (int mt = 0; mt < KT; ++mt) {
@@ -501,7 +536,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void attention_chunk_kernel(const
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) S[mt][nt] = mfma(rows, part[p][nt], S[mt][nt]);
+                    for (int nt = 0; nt < NT; ++nt) S[mt][nt] = mfma(rows, __builtin_bit_cast(v8, part[p][nt]), S[mt][nt]);
             }
         }
         if (kHalf && factor_c != 1.0f) {
