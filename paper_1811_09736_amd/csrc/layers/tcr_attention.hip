@@ -56,6 +56,7 @@ Scan scan_of(const tcr_attention& a, const View& va, const View& vb, const View&
 
 // Tokens of a sequence up to which its states stay in registers from token to token: a step costs 1.2 us, a chunk's fixed cost is 10 us.
 constexpr uint64_t kStepTokens = 8;
+constexpr uint64_t kWholeChunks = 5;
 constexpr uint64_t kFill = 512;                    // workgroups that fill the chip: two on each compute unit
 
 template <typename T, typename OUT>
@@ -82,9 +83,10 @@ ChunkShape chunk_shape(uint32_t dk, uint32_t dv) {
     return {dk <= 64 ? 64u : 128u, dv <= 64 ? 64u : 128u, 64};
 }
 
-// Memory for a call's states between blocks: the stream's workspace, or what the caller of run() sets aside.
+// Memory for a call's states between blocks: the stream's workspace, or what the caller of run() sets aside.  `turned`: the states there are
+// already those of this scan, transposed.
 struct Room {
-    bool given = false;
+    bool given = false, turned = false;
     float* floats = nullptr;
     uint64_t count = 0;
 };
@@ -99,7 +101,9 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
     Blocks b = {};
     const uint64_t span = a.offsets != nullptr ? a.total : a.tokens;
     uint64_t per_span = div_up(kFill, units * spans);
-    if (per_span > div_up(span, 2 * shape.chunk)) per_span = div_up(span, 2 * shape.chunk);
+    // (the states' and the carries' kernels take as long as a few chunks: sequences of so many stay whole)
+    const uint64_t most_blocks = span <= kWholeChunks * shape.chunk ? 1 : div_up(span, 2 * shape.chunk);
+    if (per_span > most_blocks) per_span = most_blocks;
     if (per_span > 1 && per_span * spans > most / each + 1) {
         per_span = (most / each + 1) / spans;
         if (per_span == 0) per_span = 1;
@@ -127,10 +131,13 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
     if (need != 0) {
         b.states = room.floats;
         b.keep = room.floats + (b.count - 1) * units * state_size;
-        attention_chunk_kernel<T, T, DK, W, NT, C, true><<<dim3((unsigned)((b.count - 1) * units)), dim3(64 * W), 0, stream>>>(a, b);
-        if (launched("attention_chunk_kernel<states>") != TCR_OK) return TCR_ERR_HIP;
-        attention_carry_kernel<<<dim3((unsigned)(units * state_size / 1024)), dim3(256), 0, stream>>>(b, (uint32_t)slabs, state_size);
-        if (launched("attention_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
+        b.turned = room.turned;
+        if (!room.turned) {
+            attention_chunk_kernel<T, T, DK, W, NT, C, true><<<dim3((unsigned)((b.count - 1) * units)), dim3(64 * W), 0, stream>>>(a, b);
+            if (launched("attention_chunk_kernel<states>") != TCR_OK) return TCR_ERR_HIP;
+            attention_carry_kernel<<<dim3((unsigned)(units * state_size / 256)), dim3(256), 0, stream>>>(b, (uint32_t)slabs, state_size);
+            if (launched("attention_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
+        }
     }
     attention_chunk_kernel<T, OUT, DK, W, NT, C, false><<<dim3((unsigned)(b.count * units)), dim3(64 * W), 0, stream>>>(a, b);
     return launched("attention_chunk_kernel");
@@ -221,33 +228,33 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
     of_k.st_row = 1;                     // R transposed: dv x dk
     of_k.st_col = a.dv;
     of_v.fin = dstate;
-    if (group == 1) {
-        st = run(of_k, a.dtype, false, stream);
-        return st == TCR_OK ? run(of_v, a.dtype, false, stream) : st;
-    }
-    // shared ones by way of each head's own in binary32, in front of the states in the workspace
-    const uint64_t part = div_up(of_k.total * a.heads * (a.dk > a.dv ? a.dk : a.dv), 64) * 64;
-    uint64_t states = 0, got = 0;
-    for (const Scan* r : {&of_k, &of_v}) {
-        uint64_t need = 0;
-        if (by_chunks(*r)) (void)cut(*r, chunk_shape(r->dk, r->dv), ~0ull, &need);
-        if (need > states) states = need;
-    }
-    float* floats = nullptr;
-    st = partials_for(stream, part + states, &floats, &got);
-    if (st != TCR_OK) return st;
-    if (got < part) return TCR_ERR_WORKSPACE;
+    // The states between blocks are the same for both, transposed: where both are cut alike they are worked out once.
+    // Gradients of shared keys and values go by way of each head's own in binary32, in front of the states in the workspace.
+    const uint64_t part = group == 1 ? 0 : div_up(of_k.total * a.heads * (a.dk > a.dv ? a.dk : a.dv), 64) * 64;
+    const ChunkShape shape_k = chunk_shape(of_k.dk, of_k.dv), shape_v = chunk_shape(of_v.dk, of_v.dv);
+    uint64_t need_k = 0, need_v = 0, got = 0;
+    if (by_chunks(of_k)) (void)cut(of_k, shape_k, ~0ull, &need_k);
+    if (by_chunks(of_v)) (void)cut(of_v, shape_v, ~0ull, &need_v);
     Room room;
     room.given = true;
-    room.floats = floats + part;
+    if (part + (need_k > need_v ? need_k : need_v) != 0) {
+        st = partials_for(stream, part + (need_k > need_v ? need_k : need_v), &room.floats, &got);
+        if (st != TCR_OK) return st;
+        if (got < part) return TCR_ERR_WORKSPACE;
+    }
+    float* const floats = room.floats;
+    room.floats += part;
     room.count = got - part;
-    for (Scan* r : {&of_k, &of_v}) {
+    const bool alike = need_k != 0 && need_k == need_v && shape_k.rows == shape_v.rows && shape_k.cols == shape_v.cols && shape_k.chunk == shape_v.chunk &&
+                       div_up(of_k.dv, shape_k.cols) == div_up(of_v.dv, shape_v.cols) && room.count >= need_k;
+    for (Scan* r : {&of_v, &of_k}) {
         void* const out = r->out;
-        r->out = floats;
-        st = run(*r, a.dtype, true, stream, room);
+        if (group > 1) r->out = floats;
+        room.turned = alike && r == &of_k;
+        st = run(*r, a.dtype, group > 1, stream, room);
         if (st != TCR_OK) return st;
         const uint64_t count = r->total * a.kv_heads * r->dv;
-        if (count == 0) continue;
+        if (group == 1 || count == 0) continue;
         const dim3 grid((unsigned)div_up(count, 256));
         if (a.dtype == TCR_F16) attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(floats, static_cast<_Float16*>(out), count, r->dv, group);
         else attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(floats, static_cast<__bf16*>(out), count, r->dv, group);

@@ -32,6 +32,7 @@ struct Blocks {
     uint32_t span, length, per_span, count;
     float* states;              // [heads][slabs][count - 1] of what a workgroup holds: the state behind each block but the last
     float* keep;                // [heads][count - 1]: what is left behind a block of a state in front of it
+    uint32_t turned;            // the states are transposed: those of a scan with b and c exchanged, cut alike
 };
 
 // A chunk: tokens of sequence s at rows low .. low + len - 1 of the views.
@@ -294,7 +295,21 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
 #pragma unroll
         for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[mt][nt] = *reinterpret_cast<const f4v*>(from + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
+            for (int nt = 0; nt < NT; ++nt) {
+                if (!blocks.turned) {
+                    S[mt][nt] = *reinterpret_cast<const f4v*>(from + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
+                    continue;
+                }
+                // (row k, column v of this S is row v, column k there)
+                const uint32_t v = slab * kSlab + (w * NT + nt) * 16 + n;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t k = mt * 16 + 4 * g + r;
+                    const float* there = blocks.states + ((int64_t)(h * slabs + k / kSlab) * (blocks.count - 1) + block - 1) * kStateSize +
+                                         ((k % kSlab / (16 * NT) * KT + v / 16) * NT + k / 16 % NT) * 256 + (v % 16 / 4 * 16 + k % 16) * 4 + v % 4;
+                    if (k < a.dk) S[mt][nt][r] = *there;
+                }
+            }
     }
 
     if (!STATES && a.offsets != nullptr) {
@@ -565,24 +580,24 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
     }
 }
 
-// What reaches each block from the ones in front of it: running sums over the blocks, in place.
+// What reaches each block from the ones in front of it: running sums over the blocks, in place.  A lane an element: the bytes are few, and it
+// is the wavefronts that keep enough of them on their way.
 __global__ __launch_bounds__(256) void attention_carry_kernel(const Blocks blocks, uint32_t slabs, uint64_t state_size) {
-    const uint64_t at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 4, group = at / state_size;      // (head, slab); state_size: a multiple of 1024
-    f4v* states = reinterpret_cast<f4v*>(blocks.states + group * (blocks.count - 1) * state_size + at % state_size);
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, group = at / state_size;      // (head, slab); state_size: a multiple of 256
+    float* states = blocks.states + group * (blocks.count - 1) * state_size + at % state_size;
     const float* keep = blocks.keep + group / slabs * (blocks.count - 1);
-    f4v carry = {0, 0, 0, 0};
-    // (the loads of many blocks at once, then their sums)
-    constexpr uint32_t kAtOnce = 16;
-    for (uint32_t n0 = 0; n0 + 1 < blocks.count; n0 += kAtOnce) {
-        f4v own[kAtOnce];
-        const uint32_t end = blocks.count - 1;
+    float carry = 0.0f;
+    constexpr uint32_t kAtOnce = 16;         // the loads of many blocks at once, then their sums
+    const uint32_t end = blocks.count - 1;
+    for (uint32_t n0 = 0; n0 < end; n0 += kAtOnce) {
+        float own[kAtOnce];
 #pragma unroll
-        for (uint32_t i = 0; i < kAtOnce; ++i) own[i] = states[(n0 + i < end ? n0 + i : end - 1) * (state_size / 4)];
+        for (uint32_t i = 0; i < kAtOnce; ++i) own[i] = states[(n0 + i < end ? n0 + i : end - 1) * state_size];
 #pragma unroll
         for (uint32_t i = 0; i < kAtOnce; ++i)
             if (n0 + i < end) {
-                carry = own[i] + carry * keep[n0 + i];
-                states[(n0 + i) * (state_size / 4)] = carry;
+                carry = fmaf(carry, keep[n0 + i], own[i]);
+                states[(n0 + i) * state_size] = carry;
             }
     }
 }
