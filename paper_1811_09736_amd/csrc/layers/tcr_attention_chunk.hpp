@@ -15,7 +15,8 @@
 //   S         D[dk][dv] = b^T c: operands by ds_read_b64_tr_b16, which reads 4 rows and returns columns
 //   out       D = S^T a^T + c^T P^T: a lane gets 4 consecutive elements of one token's output.  S goes from accumulator to operand
 //             without leaving its lane: the order of the 32 summands of a product is free as long as both operands have the same,
-//             so the lane's 4 + 4 rows of two tiles are summands 8g .. 8g+7, and a is read in that order.
+//             so the lane's 4 + 4 rows of two tiles are summands 8g .. 8g+7, and a is read in that order.  The tokens of b, c and P stand in
+//             the same order (4g .. 4g+3 and 16 + 4g .. 16 + 4g+3 of 32): reads of columns then meet no bank twice.
 //
 // Rounding.  The matrix cores take 16-bit operands.  a, b and c are theirs exactly; the derived ones would cost the results half of
 // their precision if they were rounded: scores and S as a factor are given as two parts (high + low, 2 products), decayed c, whose sums are the
@@ -175,10 +176,11 @@ __device__ __forceinline__ float reciprocal_power(float f) { return __builtin_bi
 
 template <typename T, int DK, int COLS, int C>
 struct ChunkLds {
-    // (rows 16 bytes beyond a multiple of 256: reads of 8 or 16 bytes from 16 rows meet no bank twice; 32 bytes: reads of columns)
-    static constexpr int kStrideA = DK + 8, kStrideB = DK + 16, kStrideC = COLS + 16, kStrideP = C + 16;
+    // (rows 16 bytes beyond a multiple of 128: reads of 8 or 16 bytes from 16 rows meet no bank twice; 32 bytes: reads of columns)
+    static constexpr int kStrideA = DK + 8, kStrideB = DK + 16, kStrideC = COLS + 16, kStrideP = C + 8;
     alignas(16) T b[C * kStrideB];
     alignas(16) T c[C * kStrideC];
+    float beyond[C];                         // (what a look-up of steps behind a short chunk's end meets, for rows of zeros)
     float powers[C + 1];                     // lambda^0 .. lambda^C
 };
 template <typename T, int DK, int COLS, int C>
@@ -242,6 +244,8 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
     }
 
     for (int i = threadIdx.x; i <= C; i += kChunkThreads) lds.powers[i] = decayed(log_decay, (float)i);
+    for (int i = threadIdx.x; i < C; i += kChunkThreads) lds.beyond[i] = 0.0f;
+    const float* const powers = lds.beyond + C;                     // powers[-C .. C]
 
     // Rows of the next chunk on their way, 16 bytes a lane.  Rows and columns beyond the ends read as 0 (an offset outside the buffer).
     constexpr int kVecs = DK / 8, kCVecs = kSlab / 8, kPassRows = kChunkThreads / kVecs, kPassRowsC = kChunkThreads / kCVecs;
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
 #pragma unroll
         for (int p = 0; p < decltype(passes)::value; ++p) {
             const int r = r0 + p * step;
-            const uint32_t at = ((uint32_t)(first + forwards * r) * tok + column) * (uint32_t)sizeof(T);
+            const uint32_t at = (__umul24((uint32_t)(first + forwards * r), tok) + column) * (uint32_t)sizeof(T);
             to[p] = __builtin_amdgcn_raw_buffer_load_b128(buffer, r < rows ? at : kOutside, 0, 0);
         }
     };
@@ -374,6 +378,8 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
 
         f4v o[CT][NT];
         if constexpr (!STATES) {
+            // (binary16: `scale` comes in with the factors at the end)
+            const float score_scale = kHalf ? 1.0f : a.out_scale;
             // ---- scores, 16 rows and 32 columns at a time, the rows by lanes
             for (int task = w; task < CT * KS; task += W) {
                 const int it = task / KS, jp = task % KS * 2;                      // (column tiles jp and jp + 1)
@@ -392,7 +398,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                     for (int r = 0; r < 4; ++r) {
                         // (a score above the diagonal is dropped, whatever it is)
                         const int steps = (it - jp - t) * 16 + n - 4 * g - r;
-                        s[t][r] = steps < 0 ? 0.0f : s[t][r] * lds.powers[steps < 0 ? 0 : steps];
+                        s[t][r] = steps < 0 ? 0.0f : s[t][r] * (powers[steps] * score_scale);
                         if constexpr (kHalf) largest = fmaxf(largest, fabsf(s[t][r]));
                     }
                 float factor = 1.0f;
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                     uint32_t x[2], y[2];
                     split<T, 2>(s[t][0] * factor, s[t][1] * factor, x, false);
                     split<T, 2>(s[t][2] * factor, s[t][3] * factor, y, false);
-                    const int at = (it * 16 + n) * SP + (jp + t) * 16 + 4 * g;
+                    const int at = (it * 16 + n) * SP + jp * 16 + 8 * g + 4 * t;
                     *reinterpret_cast<u2v*>(&lds.p[0][at]) = u2v{x[0], y[0]};
                     *reinterpret_cast<u2v*>(&lds.p[1][at]) = u2v{x[1], y[1]};
                 }
@@ -455,7 +461,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
             __syncthreads();                                                       // the scores are there
 #pragma unroll
             for (int it = 0; it < CT; ++it) {
-                float f = lds.powers[it * 16 + n + 1 - late];
+                float f = lds.powers[it * 16 + n + 1 - late] * score_scale;
                 if constexpr (kHalf) f *= reciprocal_power(factor) * lds.p_factor[it][0];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) o[it][nt] *= f;
@@ -470,7 +476,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int at = (w * NT + nt) * 16;
-                cols[ks][nt] = joined<T>(columns(lds.c, SC, ks * 32 + 8 * g, at, n), columns(lds.c, SC, ks * 32 + 8 * g + 4, at, n));
+                cols[ks][nt] = joined<T>(columns(lds.c, SC, ks * 32 + 4 * g, at, n), columns(lds.c, SC, ks * 32 + 16 + 4 * g, at, n));
                 if constexpr (kHalf)
 #pragma unroll
                     for (int r = 0; r < 8; ++r) largest_c = fmaxf(largest_c, fabsf((float)cols[ks][nt][r]));
@@ -497,14 +503,14 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
 #pragma unroll
             for (int it = 0; it < CT; ++it) {
                 const int i = it * 16 + n;
-                const float f = a.out_scale * (kHalf ? reciprocal_power(lds.p_factor[it][it / 2]) : 1.0f);
-                const uint32_t to = (uint32_t)(a.reverse ? now.len - 1 - i : i) * tok;
+                const float f = kHalf ? a.out_scale * reciprocal_power(lds.p_factor[it][it / 2]) : 1.0f;
+                const uint32_t to = __umul24((uint32_t)(a.reverse ? now.len - 1 - i : i), tok);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint32_t v = (w * NT + nt) * 16 + 4 * g;
                     const uint32_t at = i < now.len && v < left ? (to + v) * (uint32_t)sizeof(OUT) : kOutside;
                     typedef OUT o4 __attribute__((ext_vector_type(4)));
-                    const f4v x = o[it][nt] * f;
+                    const f4v x = kHalf ? o[it][nt] * f : o[it][nt];
                     const o4 y = {(OUT)x[0], (OUT)x[1], (OUT)x[2], (OUT)x[3]};
                     if constexpr (sizeof(OUT) == 2) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2v, y), out, at, 0, 0);
                     else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4v, y), out, at, 0, 0);
@@ -532,8 +538,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
             float decays[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-                const int steps = now.len - 1 - (ks * 32 + 8 * g + r);
-                decays[r] = lds.powers[steps < 0 ? 0 : steps];
+                decays[r] = powers[now.len - 1 - (ks * 32 + (r >> 2) * 16 + 4 * g + (r & 3))];
                 if constexpr (kHalf) decays[r] *= factor_c;
             }
 #pragma unroll
@@ -547,7 +552,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                 }
 #pragma unroll
             for (int mt = 0; mt < KT; ++mt) {
-                const v8 rows = joined<T>(columns(lds.b, SB, ks * 32 + 8 * g, mt * 16, n), columns(lds.b, SB, ks * 32 + 8 * g + 4, mt * 16, n));
+                const v8 rows = joined<T>(columns(lds.b, SB, ks * 32 + 4 * g, mt * 16, n), columns(lds.b, SB, ks * 32 + 16 + 4 * g, mt * 16, n));
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p)
 #pragma unroll
