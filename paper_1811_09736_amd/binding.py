@@ -145,6 +145,9 @@ def _load_native():
     _native.bind(TcrError, *(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
         "tcr_segmented_reduce", "tcr_segmented_scan_ex", "tcr_scan_ex", "tcr_reduce", "tcr_segmented_moments", "tcr_irregular_reduce",
         "tcr_irregular_scan_ex", "tcr_irregular_scan_filled", "tcr_irregular_moments")))
+    _native.bind_layers(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
+        "tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward", "tcr_rms_norm", "tcr_rms_norm_quantized",
+        "tcr_rms_norm_backward")))
     return _native
 
 
@@ -486,6 +489,10 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     q [B, T, H, dk], k [B, T, G, dk], v [B, T, G, dv], H a multiple of G; or packed sequences [N, H, dk] ... with `offsets`
     ([sequences + 1], int64).  log_decay [H], float32.  scale: dk ** -0.5 if not given.  state [sequences, H, dk, dv], float32: the
     states to go on from.  Returns out [B, T, H, dv] ([N, H, dv]), with final_state also the states behind the last tokens."""
+    if stream is None:
+        got = _native.linear_attention(q, k, v, log_decay, scale, offsets, state, final_state, out)
+        if got is not None:
+            return got
     if out is None:
         out = torch.empty(*q.shape[:-1], v.shape[-1], dtype=q.dtype, device=q.device)
     shape = _attention(q, k, v, out, log_decay, scale, offsets)
@@ -503,6 +510,10 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """tcr_linear_attention_step: one token for every sequence.  q [B, H, dk], k [B, G, dk], v [B, G, dv], state [B, H, dk, dv].
     The new states go to new_state, without it to `state` itself.  Returns out [B, H, dv]."""
+    if stream is None:
+        got = _native.linear_attention_step(q, k, v, log_decay, scale, None, state, new_state, out)
+        if got is not None:
+            return got
     if out is None:
         out = torch.empty(*q.shape[:-1], v.shape[-1], dtype=q.dtype, device=q.device)
     shape = _attention(q, k, v, out, log_decay, scale, None, step=True)
@@ -522,6 +533,10 @@ def linear_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tens
                               dfinal: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """tcr_linear_attention_backward: (dq, dk, dv, dstate) from dout and, where the final states were used, their gradient dfinal.
     dstate is None without `state`.  The decays are constants."""
+    if stream is None:
+        got = _native.linear_attention_backward(q, k, v, log_decay, scale, offsets, state, dfinal, dout)
+        if got is not None:
+            return got
     shape = _attention(q, k, v, dout, log_decay, scale, offsets)
     states = (shape.sequences, shape.heads, shape.dk, shape.dv)
     dstate = None
@@ -562,6 +577,10 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
              stream: Optional[torch.cuda.Stream] = None):
     """tcr_rms_norm over the last dimension: x * weight / sqrt(mean(x^2) + eps).  With a residual of x's shape, the norm of x +
     residual: returns (out, x + residual).  With rstd=True the reciprocal root mean square of every row (float32) comes last."""
+    if stream is None:
+        got = _native.rms_norm(x, weight, residual, eps, rstd)
+        if got is not None:
+            return got
     rows, cols = _norm_input(x, weight)
     xs, rs = _norm_rows(x, "x", x), _norm_rows(residual, "residual", x) if residual is not None else 0
     out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -577,6 +596,10 @@ def rms_norm_quantized(x: torch.Tensor, weight: torch.Tensor, residual: Optional
                        dtype: torch.dtype = torch.float8_e4m3fn, group: int = 0, stream: Optional[torch.cuda.Stream] = None):
     """tcr_rms_norm_quantized: the norm in 8 bits (float8_e4m3fn or int8) with a scale for each `group` columns (32, 64, 128; 0: for
     the row): (codes [..., cols], scales [..., groups]), with a residual (codes, scales, x + residual).  codes * scales is the norm."""
+    if stream is None and group in (0, 32, 64, 128) and dtype in (torch.float8_e4m3fn, torch.int8):
+        got = _native.rms_norm_quantized(x, weight, residual, eps, dtype is torch.int8, group)
+        if got is not None:
+            return got
     rows, cols = _norm_input(x, weight)
     if dtype not in (torch.float8_e4m3fn, torch.int8):
         raise TypeError("dtype must be torch.float8_e4m3fn or torch.int8")
@@ -595,6 +618,10 @@ def rms_norm_backward(dout: torch.Tensor, total: torch.Tensor, weight: torch.Ten
                       stream: Optional[torch.cuda.Stream] = None):
     """tcr_rms_norm_backward: (dx, dweight) from rms_norm's x + residual (its x, without a residual) and rstd; dtotal: the gradient
     of x + residual itself, added.  dx is the gradient of x and of the residual alike."""
+    if stream is None:
+        got = _native.rms_norm_backward(dout, total, weight, rstd, dtotal)
+        if got is not None:
+            return got
     rows, cols = _norm_input(total, weight)
     ds, ts = _norm_rows(dout, "dout", total), _norm_rows(total, "total", total)
     ms = _norm_rows(dtotal, "dtotal", total) if dtotal is not None else 0

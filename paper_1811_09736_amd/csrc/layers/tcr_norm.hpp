@@ -45,6 +45,15 @@ template <> struct Vec<_Float16> { typedef _Float16 v __attribute__((ext_vector_
 template <> struct Vec<__bf16> { typedef __bf16 v __attribute__((ext_vector_type(8), aligned(2))); };
 template <> struct Vec<float> { typedef float v __attribute__((ext_vector_type(8), aligned(4))); };
 
+// The same as they are in memory.
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::v load_raw(const T* row, uint64_t col, uint64_t cols) {
+    if (col + kVec <= cols) return *reinterpret_cast<const typename Vec<T>::v*>(row + col);
+    typename Vec<T>::v x;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) x[i] = col + i < cols ? row[col + i] : (T)0.0f;
+    return x;
+}
 // Columns col .. col + 7 of a row, 0 beyond its end.
 template <typename T>
 __device__ __forceinline__ void load_vec(const T* row, uint64_t col, uint64_t cols, float (&v)[kVec]) {
@@ -76,11 +85,6 @@ __device__ __forceinline__ void load_weight(const void* w, uint32_t wide, uint64
     else load_vec(static_cast<const T*>(w), col, cols, v);
 }
 
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    return x;
-}
 // The larger magnitude; NaN, whose bits are the largest, stays.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
@@ -90,29 +94,39 @@ __device__ __forceinline__ uint32_t lanes_largest(uint32_t x) {
     for (int m = 1; m < LANES; m <<= 1) x = larger(x, (uint32_t)__shfl_xor((int)x, m));
     return x;
 }
-// The sum (maximum) over the WAVES wavefronts of a workgroup, each wavefront's own given.  `sums` is free again only after the
-// next barrier.
-template <int WAVES>
-__device__ __forceinline__ float block_sum(float x, float* sums) {
-    x = wave_sum(x);
-    if constexpr (WAVES == 1) return x;
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float total = 0.0f;
+// The sum (maximum) over what holds a row: LANES lanes of a wavefront (<= 64), or all wavefronts of the workgroup (0).  `room` is free again
+// only after the next barrier.
+template <int LANES>
+__device__ __forceinline__ float row_sum(float x, float* room) {
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) total += sums[w];
-    return total;
+    for (int m = 1; m < (LANES == 0 ? 64 : LANES); m <<= 1) x += __shfl_xor(x, m);
+    if constexpr (LANES == 0) {
+        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = 0.0f;
+        for (uint32_t w = 0; w < blockDim.x / 64; ++w) x += room[w];
+    }
+    return x;
 }
-template <int WAVES>
-__device__ __forceinline__ uint32_t block_largest(uint32_t x, uint32_t* most) {
-    x = lanes_largest<64>(x);
-    if constexpr (WAVES == 1) return x;
-    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = x;
-    __syncthreads();
-    uint32_t all = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) all = larger(all, most[w]);
-    return all;
+template <int LANES>
+__device__ __forceinline__ uint32_t row_largest(uint32_t x, uint32_t* room) {
+    x = lanes_largest<LANES == 0 ? 64 : LANES>(x);
+    if constexpr (LANES == 0) {
+        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = 0;
+        for (uint32_t w = 0; w < blockDim.x / 64; ++w) x = larger(x, room[w]);
+    }
+    return x;
+}
+// The largest magnitude of a group of columns, which 4, 8 or 16 lanes hold (a row starts on a group; lanes beyond its end hold zeros; fewer
+// lanes than a group's hold a whole row).
+template <int LANES>
+__device__ __forceinline__ uint32_t group_largest(uint32_t x, uint32_t group) {
+    x = lanes_largest<4>(x);
+    if (group >= 64) x = larger(x, (uint32_t)__shfl_xor((int)x, 4));
+    if (group >= 128 && LANES != 8) x = larger(x, (uint32_t)__shfl_xor((int)x, 8));
+    return x;
 }
 
 template <int OUT>
@@ -147,44 +161,47 @@ __device__ __forceinline__ void store_codes(uint8_t* row, uint64_t col, uint64_t
     }
 }
 
-// WAVES wavefronts per row, ITEMS vectors per lane: rows of up to WAVES * 64 * ITEMS * 8 columns.
-template <typename T, int OUT, int WAVES, int ITEMS>
-__global__ __launch_bounds__(WAVES * 64) void norm_kernel(const Norm a) {
-    constexpr int kLanes = WAVES * 64;
-    __shared__ float sums[WAVES];
-    __shared__ uint32_t most[WAVES];
-    const uint64_t row = blockIdx.x, cols = a.cols;
+// ITEMS vectors per lane; LANES lanes per row and 256 / LANES rows per workgroup, or (0) a row per workgroup, of as many wavefronts as hold it.
+// MI355X: 16384 x 4096 bfloat16 with the residual, 537 MB, in 90 us, 6.0 TB/s: what a copy reaches.
+constexpr int kNormThreads = 256, kMostWaves = 16;
+template <typename T, int OUT, int LANES, int ITEMS>
+__global__ __launch_bounds__(LANES == 0 ? kMostWaves * 64 : kNormThreads) void norm_kernel(const Norm a) {
+    __shared__ float sums[kMostWaves];
+    __shared__ uint32_t most[kMostWaves];
+    const uint32_t lanes = LANES == 0 ? blockDim.x : LANES, lane = LANES == 0 ? threadIdx.x : threadIdx.x % LANES;
+    const uint64_t row = LANES == 0 ? blockIdx.x : (uint64_t)blockIdx.x * (kNormThreads / (LANES == 0 ? 1 : LANES)) + threadIdx.x / (LANES == 0 ? 1 : LANES);
+    if (row >= a.rows) return;                            // (whole groups of lanes, in kernels without barriers)
+    const uint64_t cols = a.cols;
     const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
     const T* r = a.residual != nullptr ? static_cast<const T*>(a.residual) + (int64_t)row * a.r_stride : nullptr;
 
-    float s[ITEMS][kVec];
+    typename Vec<T>::v first[ITEMS], second[ITEMS];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) load_vec(x, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, s[i]);
+    for (int i = 0; i < ITEMS; ++i) first[i] = load_raw(x, ((uint64_t)i * lanes + lane) * kVec, cols);
     if (r != nullptr) {
-        float add[ITEMS][kVec];
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) load_vec(r, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, add[i]);
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) s[i][j] += add[i][j];
+        for (int i = 0; i < ITEMS; ++i) second[i] = load_raw(r, ((uint64_t)i * lanes + lane) * kVec, cols);
     }
-    float square = 0.0f;
+    float s[ITEMS][kVec], square = 0.0f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) square = fmaf(s[i][j], s[i][j], square);
-    const float rstd = 1.0f / sqrtf(block_sum<WAVES>(square, sums) / (float)cols + a.eps);
-    if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
+        for (int j = 0; j < kVec; ++j) {
+            s[i][j] = (float)first[i][j];
+            if (r != nullptr) s[i][j] += (float)second[i][j];
+            square = fmaf(s[i][j], s[i][j], square);
+        }
+    const float rstd = 1.0f / sqrtf(row_sum<LANES>(square, sums) / (float)cols + a.eps);
+    if (a.rstd != nullptr && lane == 0) a.rstd[row] = rstd;
     if (a.total != nullptr) {
         T* total = static_cast<T*>(a.total) + row * cols;
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) store_vec(total, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, s[i]);
+        for (int i = 0; i < ITEMS; ++i) store_vec(total, ((uint64_t)i * lanes + lane) * kVec, cols, s[i]);
     }
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+        const uint64_t col = ((uint64_t)i * lanes + lane) * kVec;
         float w[kVec];
         load_weight<T>(a.weight, a.weight_wide, col, cols, w);
 #pragma unroll
@@ -195,11 +212,7 @@ __global__ __launch_bounds__(WAVES * 64) void norm_kernel(const Norm a) {
         if constexpr (OUT == kNormSame) {
             store_vec(static_cast<T*>(a.out) + row * cols, col, cols, s[i]);
         } else if (a.group != 0) {
-            // 4, 8 or 16 lanes hold a group (the row starts on a group, and lanes beyond its end hold zeros)
-            uint32_t g = lanes_largest<4>(top);
-            if (a.group >= 64) g = larger(g, (uint32_t)__shfl_xor((int)g, 4));
-            if (a.group >= 128) g = larger(g, (uint32_t)__shfl_xor((int)g, 8));
-            const float scale = scale_of<OUT>(g);
+            const float scale = scale_of<OUT>(group_largest<LANES>(top, a.group));
             if (col < cols) {
                 store_codes(static_cast<uint8_t*>(a.out) + row * cols, col, cols, codes_of<OUT>(s[i], 1.0f / scale));
                 if (col % a.group == 0) a.scales[row * ((cols + a.group - 1) / a.group) + col / a.group] = scale;
@@ -209,11 +222,11 @@ __global__ __launch_bounds__(WAVES * 64) void norm_kernel(const Norm a) {
     }
     if constexpr (OUT != kNormSame) {
         if (a.group == 0) {
-            const float scale = scale_of<OUT>(block_largest<WAVES>(top, most));
-            if (threadIdx.x == 0) a.scales[row] = scale;
+            const float scale = scale_of<OUT>(row_largest<LANES>(top, most));
+            if (lane == 0) a.scales[row] = scale;
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+                const uint64_t col = ((uint64_t)i * lanes + lane) * kVec;
                 if (col < cols) store_codes(static_cast<uint8_t*>(a.out) + row * cols, col, cols, codes_of<OUT>(s[i], 1.0f / scale));
             }
         }
@@ -221,7 +234,7 @@ __global__ __launch_bounds__(WAVES * 64) void norm_kernel(const Norm a) {
 }
 
 // Rows that no registers hold: the row is read again for each use (from a cache, mostly).
-constexpr int kLongWaves = 16;
+constexpr int kLongWaves = kMostWaves;
 template <typename T, int OUT>
 __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a) {
     constexpr uint64_t kStep = kLongWaves * 64 * kVec;
@@ -244,7 +257,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a
 #pragma unroll
         for (int j = 0; j < kVec; ++j) square = fmaf(s[j], s[j], square);
     }
-    const float rstd = 1.0f / sqrtf(block_sum<kLongWaves>(square, sums) / (float)cols + a.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<0>(square, sums) / (float)cols + a.eps);
     if (a.rstd != nullptr && threadIdx.x == 0) a.rstd[row] = rstd;
     float scale = 1.0f;
     if constexpr (OUT != kNormSame) {
@@ -256,7 +269,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a
 #pragma unroll
                 for (int j = 0; j < kVec; ++j) top = larger(top, magnitude(s[j] * rstd * w[j]));
             }
-            scale = scale_of<OUT>(block_largest<kLongWaves>(top, most));
+            scale = scale_of<OUT>(row_largest<0>(top, most));
             if (threadIdx.x == 0) a.scales[row] = scale;
         }
     }
@@ -277,10 +290,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a
             store_vec(static_cast<T*>(a.out) + row * cols, col, cols, s);
         } else {
             if (a.group != 0) {
-                uint32_t g = lanes_largest<4>(top);
-                if (a.group >= 64) g = larger(g, (uint32_t)__shfl_xor((int)g, 4));
-                if (a.group >= 128) g = larger(g, (uint32_t)__shfl_xor((int)g, 8));
-                scale = scale_of<OUT>(g);
+                scale = scale_of<OUT>(group_largest<0>(top, a.group));
                 if (col < cols && col % a.group == 0) a.scales[row * ((cols + a.group - 1) / a.group) + col / a.group] = scale;
             }
             if (col < cols) store_codes(static_cast<uint8_t*>(a.out) + row * cols, col, cols, codes_of<OUT>(s, 1.0f / scale));
@@ -288,28 +298,49 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a
     }
 }
 
-// Gradients: a workgroup takes every parts-th row and keeps its sums of dweight in registers.
-template <typename T, int WAVES, int ITEMS>
-__global__ __launch_bounds__(WAVES * 64) void norm_grad_kernel(const NormGrad a) {
-    constexpr int kLanes = WAVES * 64;
-    __shared__ float sums[2][WAVES];
+// Gradients: a row per wavefront and four per workgroup (LANES == 64), or a row per workgroup (0); each takes every parts-th of them, the next
+// row's loads on their way meanwhile, and keeps its sums of dweight in registers.
+template <typename T, int LANES, int ITEMS>
+__global__ __launch_bounds__(LANES == 0 ? kMostWaves * 64 : kNormThreads) void norm_grad_kernel(const NormGrad a) {
+    static_assert(LANES == 0 || LANES == 64, "");
+    constexpr uint32_t kRowsAtOnce = LANES == 0 ? 1 : kNormThreads / 64;
+    __shared__ float sums[2][kMostWaves];
+    __shared__ float parts[LANES == 0 ? 1 : kRowsAtOnce][LANES == 0 ? 1 : 64 * kVec * ITEMS];
+    const uint32_t lanes = LANES == 0 ? blockDim.x : LANES, lane = LANES == 0 ? threadIdx.x : threadIdx.x % 64, in_group = LANES == 0 ? 0 : threadIdx.x / 64;
     const uint64_t cols = a.cols;
+    typedef typename Vec<T>::v vec;
     float dw[ITEMS][kVec] = {};
-    int turn = 0;
-    for (uint64_t row = blockIdx.x; row < a.rows; row += a.parts, turn ^= 1) {
-        const T* dy = static_cast<const T*>(a.dout) + (int64_t)row * a.dout_stride;
-        const T* total = static_cast<const T*>(a.total) + (int64_t)row * a.total_stride;
-        const float rstd = a.rstd[row];
-        float g[ITEMS][kVec], s[ITEMS][kVec], dot = 0.0f;
+    vec dy[ITEMS], total[ITEMS], more[ITEMS];
+    auto load = [&](uint64_t row) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
-            load_vec(dy, col, cols, g[i]);
-            load_vec(total, col, cols, s[i]);
+            const uint64_t col = ((uint64_t)i * lanes + lane) * kVec;
+            dy[i] = load_raw(static_cast<const T*>(a.dout) + (int64_t)row * a.dout_stride, col, cols);
+            total[i] = load_raw(static_cast<const T*>(a.total) + (int64_t)row * a.total_stride, col, cols);
+            if (a.dtotal != nullptr) more[i] = load_raw(static_cast<const T*>(a.dtotal) + (int64_t)row * a.dtotal_stride, col, cols);
         }
+    };
+    constexpr bool kAhead = ITEMS == 1;                   // (two vectors a lane leave no registers for the next row's)
+    const uint64_t step = (uint64_t)a.parts * kRowsAtOnce;
+    uint64_t row = (uint64_t)blockIdx.x * kRowsAtOnce + in_group;
+    if (kAhead && row < a.rows) load(row);
+    for (int turn = 0; row < a.rows; turn ^= 1) {
+        if (!kAhead) load(row);
+        const float rstd = a.rstd[row];
+        float g[ITEMS][kVec], s[ITEMS][kVec], add[ITEMS][kVec], dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                g[i][j] = (float)dy[i][j];
+                s[i][j] = (float)total[i][j];
+                add[i][j] = a.dtotal != nullptr ? (float)more[i][j] : 0.0f;
+            }
+        const uint64_t next = row + step;
+        if (kAhead && next < a.rows) load(next);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
+            const uint64_t col = ((uint64_t)i * lanes + lane) * kVec;
             float w[kVec];
             load_weight<T>(a.weight, a.weight_wide, col, cols, w);
 #pragma unroll
@@ -320,21 +351,32 @@ __global__ __launch_bounds__(WAVES * 64) void norm_grad_kernel(const NormGrad a)
             }
         }
         // (two places for the sums: a wavefront that is a row ahead writes to the other one)
-        const float c = block_sum<WAVES>(dot, sums[turn]) / (float)cols * rstd * rstd;
+        const float c = row_sum<LANES>(dot, sums[turn]) / (float)cols * rstd * rstd;
         T* dx = static_cast<T*>(a.dx) + row * cols;
-        const T* more = a.dtotal != nullptr ? static_cast<const T*>(a.dtotal) + (int64_t)row * a.dtotal_stride : nullptr;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const uint64_t col = ((uint64_t)i * kLanes + threadIdx.x) * kVec;
-            float add[kVec] = {};
-            if (more != nullptr) load_vec(more, col, cols, add);
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) g[i][j] = fmaf(rstd, g[i][j] - s[i][j] * c, add[j]);
-            store_vec(dx, col, cols, g[i]);
+            for (int j = 0; j < kVec; ++j) g[i][j] = fmaf(rstd, g[i][j] - s[i][j] * c, add[i][j]);
+            store_vec(dx, ((uint64_t)i * lanes + lane) * kVec, cols, g[i]);
+        }
+        row = next;
+    }
+    if constexpr (LANES == 0) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) store_vec(a.part + (uint64_t)blockIdx.x * cols, ((uint64_t)i * lanes + lane) * kVec, cols, dw[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) parts[in_group][(i * 64 + lane) * kVec + j] = dw[i][j];
+        __syncthreads();
+        for (uint32_t col = threadIdx.x; col < cols; col += kNormThreads) {
+            float sum = 0.0f;
+#pragma unroll
+            for (uint32_t r = 0; r < kRowsAtOnce; ++r) sum += parts[r][col];
+            a.part[(uint64_t)blockIdx.x * cols + col] = sum;
         }
     }
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) store_vec(a.part + (uint64_t)blockIdx.x * cols, ((uint64_t)i * kLanes + threadIdx.x) * kVec, cols, dw[i]);
 }
 
 // The same for rows that no registers hold: dx here, dweight in norm_weight_kernel.
@@ -360,7 +402,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_grad_long_kernel(const N
 #pragma unroll
         for (int j = 0; j < kVec; ++j) dot = fmaf(g[j], s[j], dot);
     }
-    const float c = block_sum<kLongWaves>(dot, sums) / (float)cols * rstd * rstd;
+    const float c = row_sum<0>(dot, sums) / (float)cols * rstd * rstd;
     for (uint64_t col = threadIdx.x * kVec; col < cols; col += kStep) {
         load(col);
         float add[kVec] = {};
@@ -395,7 +437,7 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float* __restric
     const int wave = threadIdx.x >> 6;
     float sum = 0.0f;
     if (col < cols) {
-#pragma unroll 8
+#pragma unroll 16
         for (uint32_t p = wave; p < parts; p += 16) sum += part[(uint64_t)p * cols + col];
     }
     sums[wave][threadIdx.x & 63] = sum;

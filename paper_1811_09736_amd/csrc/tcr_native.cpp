@@ -17,6 +17,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+
 #include "../../include/tcr.h"
 
 namespace {
@@ -264,9 +266,13 @@ PyObject* bind(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
+#include "layers/tcr_native_layers.hpp"
+
 #define TCR_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {TCR_FAST(segmented_reduce), TCR_FAST(segmented_scan), TCR_FAST(scan), TCR_FAST(reduce), TCR_FAST(segmented_moments),
                            TCR_FAST(irregular_reduce), TCR_FAST(irregular_moments), TCR_FAST(irregular_scan),
+                           TCR_FAST(linear_attention), TCR_FAST(linear_attention_step), TCR_FAST(linear_attention_backward), TCR_FAST(rms_norm),
+                           TCR_FAST(rms_norm_quantized), TCR_FAST(rms_norm_backward), {"bind_layers", bind_layers, METH_VARARGS, nullptr},
                            {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "The ordinary calls of binding.py (see there).", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -363,6 +363,8 @@ def test_long_offsets_beyond_32_bits(tcr):
         far.append(w)
     want = tcr.linear_attention(q, k, v, decay, state=s)
     assert torch.equal(tcr.linear_attention(*far, decay, state=s), want)
+    del far, room, w
+    torch.cuda.empty_cache()                 # (12 GiB that later tests in this process may want to see free)
 
 
 def test_refusals(tcr):
