@@ -190,14 +190,18 @@ struct ChunkLdsOut : ChunkLds<T, DK, COLS, C> {
     float p_factor[C / 16][C / 32];          // of the scores of 16 rows and 32 columns
 };
 
-// A range of memory of whose 2^31 bytes what lies outside reads as 0 and is not written (kOutside).
-constexpr uint32_t kOutside = 0xfffffff0u;
+// What is loaded in front of this is asked for in front of it.  (Left to itself the compiler asks for each operand right where it is used, and waits for
+// every one: a chunk took twice as long.)
+__device__ __forceinline__ void loads_first() { __builtin_amdgcn_sched_barrier(0); }
+
+// A range of memory of whose 2^31 bytes what lies outside reads as 0 and is not written: kOutside does, also with a scalar offset added.
+constexpr uint32_t kOutside = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(uniform(p)), 0, 0x7fffffff, 0x00020000);
 }
 
 template <typename T, typename OUT, int DK, int W, int NT, int C, bool STATES>
-__global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Scan a, const Blocks blocks) {
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W / 2))) void attention_chunk_kernel(const Scan a, const Blocks blocks) {
     typedef typename Bits<T>::v8 v8;
     constexpr bool kHalf = std::is_same<T, _Float16>::value;
     constexpr int CT = C / 16, KT = DK / 16, kParts = kHalf ? 2 : 3, kSlab = 16 * W * NT, KS = C / 32;
@@ -247,27 +251,30 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
     for (int i = threadIdx.x; i < C; i += kChunkThreads) lds.beyond[i] = 0.0f;
     const float* const powers = lds.beyond + C;                     // powers[-C .. C]
 
-    // Rows of the next chunk on their way, 16 bytes a lane.  Rows and columns beyond the ends read as 0 (an offset outside the buffer).
+    // Rows of the next chunk on their way, 16 bytes a lane.  Rows and columns beyond the ends read as 0 (an offset outside the buffer).  A lane's
+    // rows are `step` apart, so one offset serves all of its loads; backwards they count down from the last of C rows.
     constexpr int kVecs = DK / 8, kCVecs = kSlab / 8, kPassRows = kChunkThreads / kVecs, kPassRowsC = kChunkThreads / kCVecs;
     constexpr int kPasses = C / kPassRows, kPassesC = C / kPassRowsC;
     u4v ra[kPasses], rb[kPasses], rc[kPassesC];
-    int row = threadIdx.x / kVecs, col = threadIdx.x % kVecs * 8, row_c = threadIdx.x / kCVecs, col_c = threadIdx.x % kCVecs * 8;
-    const int forwards = a.reverse ? -1 : 1;
-    auto fetch = [&](const T* head, const View& v, const Chunk& c, int r0, bool inside, uint32_t column, int step, u4v* to, auto passes) {
-        const uint32_t tok = (uint32_t)v.tok;
-        const __amdgpu_buffer_rsrc_t buffer = buffer_at(head + ((a.offsets == nullptr ? (int64_t)c.s * v.seq : 0) + (int64_t)c.low * tok));
-        const int rows = inside ? c.len : 0, first = a.reverse ? c.len - 1 : 0;
+    uint32_t row = threadIdx.x / kVecs, col = threadIdx.x % kVecs * 8, row_c = threadIdx.x / kCVecs, col_c = threadIdx.x % kCVecs * 8;
+    const uint32_t tok_a = (uint32_t)a.a.tok, tok_b = (uint32_t)a.b.tok, tok_c = (uint32_t)a.c.tok, tok_o = (uint32_t)a.out_tok;
+    const bool reverse = a.reverse != 0;
+    auto fetch = [&](const T* head, int64_t seq, uint32_t tok, const Chunk& c, uint32_t r0, uint32_t column, bool inside, auto step, u4v* to, auto passes) {
+        constexpr int kStep = decltype(step)::value, kCount = decltype(passes)::value;
+        const int64_t first = (int64_t)c.low + (reverse ? c.len - C : 0);                    // (maybe in front of the array; no such row is read)
+        const __amdgpu_buffer_rsrc_t buffer = buffer_at(head + ((int64_t)c.s * seq + first * (int64_t)tok));
+        const uint32_t at = (__umul24(reverse ? C - 1 - (kCount - 1) * kStep - r0 : r0, tok) + column) * (uint32_t)sizeof(T);
+        const uint32_t pitch = kStep * tok * (uint32_t)sizeof(T), rows = inside ? (uint32_t)c.len : 0u;
 #pragma unroll
-        for (int p = 0; p < decltype(passes)::value; ++p) {
-            const int r = r0 + p * step;
-            const uint32_t at = (__umul24((uint32_t)(first + forwards * r), tok) + column) * (uint32_t)sizeof(T);
-            to[p] = __builtin_amdgcn_raw_buffer_load_b128(buffer, r < rows ? at : kOutside, 0, 0);
-        }
+        for (int p = 0; p < kCount; ++p)
+            to[p] = __builtin_amdgcn_raw_buffer_load_b128(buffer, r0 + p * kStep < rows ? at : kOutside, (reverse ? kCount - 1 - p : p) * pitch, 0);
     };
     auto fetch_all = [&](const Chunk& c) {
-        if constexpr (!STATES) fetch(pa, a.a, c, row, (uint32_t)col < a.dk, col, kPassRows, ra, std::integral_constant<int, kPasses>());
-        fetch(pb, a.b, c, row, (uint32_t)col < a.dk, col, kPassRows, rb, std::integral_constant<int, kPasses>());
-        fetch(pc, a.c, c, row_c, (uint32_t)col_c < left, col_c, kPassRowsC, rc, std::integral_constant<int, kPassesC>());
+        const std::integral_constant<int, kPassRows> step;
+        const std::integral_constant<int, kPasses> passes;
+        if constexpr (!STATES) fetch(pa, a.a.seq, tok_a, c, row, col, col < a.dk, step, ra, passes);
+        fetch(pb, a.b.seq, tok_b, c, row, col, col < a.dk, step, rb, passes);
+        fetch(pc, a.c.seq, tok_c, c, row_c, col_c, col_c < left, std::integral_constant<int, kPassRowsC>(), rc, std::integral_constant<int, kPassesC>());
     };
 
     // S: rows 16 mt + 4 g + r, columns 16 (NT w + nt) + n of the slab
@@ -283,7 +290,8 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
         uint32_t k0 = 4 * g, v0 = w * 16 * NT + n;
         const uint32_t st_row = (uint32_t)a.st_row, st_col = (uint32_t)a.st_col;
 #pragma unroll
-        for (int mt = 0; mt < KT; ++mt)
+        for (int mt = 0; mt < KT; ++mt) {
+            __builtin_amdgcn_sched_barrier(0);                      // (few offsets at a time)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -291,6 +299,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                     const uint32_t k = k0 + mt * 16 + r, v = v0 + 16 * nt;
                     S[mt][nt][r] = f(S[mt][nt][r], k < a.dk && v < left ? (k * st_row + (v + slab * kSlab) * st_col) * 4 : kOutside);
                 }
+        }
     };
     float* const own_states = blocks.states + ((int64_t)(h * slabs + slab) * (blocks.count - 1) + block) * kStateSize;
     clear();
@@ -345,9 +354,9 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
     while (more) {
         // (addresses are worked out in every chunk: kept in registers all along they would push others to memory, and the wait for one of those
         // is a wait for the next chunk's rows too)
-        int t = threadIdx.x;
+        uint32_t t = threadIdx.x;
         asm volatile("" : "+v"(t));
-        lane = t & 63;
+        lane = (int)(t & 63);
         n = lane & 15;
         g = lane >> 4;
         row = t / kVecs;
@@ -385,11 +394,26 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                 const int it = task / KS, jp = task % KS * 2;                      // (column tiles jp and jp + 1)
                 if (jp > it) continue;
                 f4v s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                const bool both = jp < it;
+                constexpr int kAhead = W == 8 ? (kHalf ? 1 : 2) : 4;                             // (products' operands at once: as registers allow)
 #pragma unroll
-                for (int ks = 0; ks < DK / 32; ++ks) {
-                    const v8 rows = *reinterpret_cast<const v8*>(&lds.a[(it * 16 + n) * SA + ks * 32 + 8 * g]);
-                    s[0] = mfma(*reinterpret_cast<const v8*>(&lds.b[(jp * 16 + n) * SB + ks * 32 + 8 * g]), rows, s[0]);
-                    if (jp < it) s[1] = mfma(*reinterpret_cast<const v8*>(&lds.b[(jp * 16 + 16 + n) * SB + ks * 32 + 8 * g]), rows, s[1]);
+                for (int k0 = 0; k0 < DK / 32; k0 += kAhead) {
+                    v8 rows[kAhead], by[2][kAhead];
+#pragma unroll
+                    for (int ks = 0; ks < kAhead; ++ks) {
+                        if (k0 + ks >= DK / 32) continue;
+                        const int at = (k0 + ks) * 32 + 8 * g;
+                        rows[ks] = *reinterpret_cast<const v8*>(&lds.a[(it * 16 + n) * SA + at]);
+                        by[0][ks] = *reinterpret_cast<const v8*>(&lds.b[(jp * 16 + n) * SB + at]);
+                        by[1][ks] = *reinterpret_cast<const v8*>(&lds.b[(jp * 16 + 16 + n) * SB + at]);
+                    }
+                    loads_first();
+#pragma unroll
+                    for (int ks = 0; ks < kAhead; ++ks) {
+                        if (k0 + ks >= DK / 32) continue;
+                        s[0] = mfma(by[0][ks], rows[ks], s[0]);
+                        if (both) s[1] = mfma(by[1][ks], rows[ks], s[1]);
+                    }
                 }
                 float largest = 0.0f;
 #pragma unroll
@@ -440,6 +464,7 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                     const T* from = &lds.a[(it * 16 + n) * SA + ks * 32 + 4 * g];
                     rows[it] = joined<T>(*reinterpret_cast<const s4v*>(from), *reinterpret_cast<const s4v*>(from + 16));
                 }
+                if (!(kHalf && W == 8)) loads_first();
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     u4v parts[2];
@@ -482,33 +507,46 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                     for (int r = 0; r < 8; ++r) largest_c = fmaxf(largest_c, fabsf((float)cols[ks][nt][r]));
             }
         if constexpr (!STATES) {
+            constexpr bool kNextToo = W != 8;                                      // (as registers allow)
+            v8 scores[2][CT];                                                      // one part of 32 columns, and the next on its way
+            auto read_scores = [&](int at) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+                for (int it = at / 2 * 2; it < CT; ++it)
+                    scores[at & 1][it] = *reinterpret_cast<const v8*>(&lds.p[at & 1][(it * 16 + n) * SP + at / 2 * 32 + 8 * g]);
+            };
+            if (kNextToo) read_scores(0);
+#pragma unroll
+            for (int at = 0; at < 2 * KS; ++at) {
+                const int ks = at / 2;
+                if (!kNextToo) read_scores(at);
+                else if (at + 1 < 2 * KS) read_scores(at + 1);
+                loads_first();
 #pragma unroll
                 for (int it = 2 * ks; it < CT; ++it) {
-                    if (kHalf && ks > 0) {                                         // from the factor of the columns in front to these
+                    if (kHalf && ks > 0 && (at & 1) == 0) {                        // from the factor of the columns in front to these
                         const float f = lds.p_factor[it][ks] * reciprocal_power(lds.p_factor[it][ks - 1]);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) o[it][nt] *= f;
                     }
 #pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        const v8 scores = *reinterpret_cast<const v8*>(&lds.p[part][(it * 16 + n) * SP + ks * 32 + 8 * g]);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) o[it][nt] = mfma(cols[ks][nt], scores, o[it][nt]);
-                    }
+                    for (int nt = 0; nt < NT; ++nt) o[it][nt] = mfma(cols[ks][nt], scores[at & 1][it], o[it][nt]);
                 }
-            const uint32_t tok = (uint32_t)a.out_tok;
-            const __amdgpu_buffer_rsrc_t out = buffer_at(po + ((a.offsets == nullptr ? (int64_t)now.s * a.out_seq : 0) + (int64_t)now.low * tok));
+            }
+            // (rows 16 it + n; backwards from the last of C, as above)
+            const int64_t first = (int64_t)now.low + (reverse ? now.len - C : 0);
+            const __amdgpu_buffer_rsrc_t out = buffer_at(po + ((int64_t)now.s * a.out_seq + first * (int64_t)tok_o));
+            const uint32_t pitch = 16 * tok_o * (uint32_t)sizeof(OUT);
+            const uint32_t at_row = __umul24((uint32_t)(reverse ? 15 - n : n), tok_o);
 #pragma unroll
             for (int it = 0; it < CT; ++it) {
-                const int i = it * 16 + n;
                 const float f = kHalf ? a.out_scale * reciprocal_power(lds.p_factor[it][it / 2]) : 1.0f;
-                const uint32_t to = __umul24((uint32_t)(a.reverse ? now.len - 1 - i : i), tok);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint32_t v = (w * NT + nt) * 16 + 4 * g;
-                    const uint32_t at = i < now.len && v < left ? (to + v) * (uint32_t)sizeof(OUT) : kOutside;
+                    // (the tile's offset is added here and not given as the store's scalar one: 16-byte stores of that form lost their first
+                    // elements to the instructions behind them in a few lanes)
+                    const uint32_t behind = (reverse ? CT - 1 - it : it) * pitch;
+                    const uint32_t at = it * 16 + n < now.len && v < left ? (at_row + v) * (uint32_t)sizeof(OUT) + behind : kOutside;
                     typedef OUT o4 __attribute__((ext_vector_type(4)));
                     const f4v x = kHalf ? o[it][nt] * f : o[it][nt];
                     const o4 y = {(OUT)x[0], (OUT)x[1], (OUT)x[2], (OUT)x[3]};
@@ -534,6 +572,13 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
         }
 #pragma unroll
         for (int ks = 0; ks < C / 32; ++ks) {
+            constexpr int kBatch = W == 8 ? (kHalf ? 2 : 4) : (KT < 8 ? 4 : 8);
+            v8 rows[kBatch];
+            auto read_rows = [&](int m0) {
+#pragma unroll
+                for (int m = 0; m < kBatch; ++m)
+                    rows[m] = joined<T>(columns(lds.b, SB, ks * 32 + 4 * g, (m0 + m) * 16, n), columns(lds.b, SB, ks * 32 + 16 + 4 * g, (m0 + m) * 16, n));
+            };
             u4v part[kParts][NT];
             float decays[8];
 #pragma unroll
@@ -541,6 +586,8 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                 decays[r] = powers[now.len - 1 - (ks * 32 + (r >> 2) * 16 + 4 * g + (r & 3))];
                 if constexpr (kHalf) decays[r] *= factor_c;
             }
+            read_rows(0);
+            loads_first();
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -551,12 +598,17 @@ __global__ __launch_bounds__(64 * W, W / 2) void attention_chunk_kernel(const Sc
                     for (int p = 0; p < kParts; ++p) part[p][nt][r] = y[p];
                 }
 #pragma unroll
-            for (int mt = 0; mt < KT; ++mt) {
-                const v8 rows = joined<T>(columns(lds.b, SB, ks * 32 + 4 * g, mt * 16, n), columns(lds.b, SB, ks * 32 + 16 + 4 * g, mt * 16, n));
+            for (int m0 = 0; m0 < KT; m0 += kBatch) {
+                if (m0 > 0) {
+                    read_rows(m0);
+                    loads_first();
+                }
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) S[mt][nt] = mfma(rows, __builtin_bit_cast(v8, part[p][nt]), S[mt][nt]);
+                    for (int m = 0; m < kBatch; ++m)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) S[m0 + m][nt] = mfma(rows[m], __builtin_bit_cast(v8, part[p][nt]), S[m0 + m][nt]);
             }
         }
         if (kHalf && factor_c != 1.0f) {

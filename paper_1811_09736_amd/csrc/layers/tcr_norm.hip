@@ -12,8 +12,8 @@ namespace {
 
 constexpr uint64_t kMostRows = 1ull << 31, kMostCols = 1ull << 24;
 
-// Lanes of 8 columns for a row of up to 512, several rows a workgroup; then a workgroup of as many wavefronts as hold the row with 8 columns a lane, or
-// with 16: a row of 5120 columns takes 10 wavefronts and none idles (8 of 16 columns a lane, the next power of two, read 4.6 TB/s instead of 5.3).
+// Lanes of 8 columns for a row of up to 512, several rows a workgroup; then a workgroup of as many wavefronts as hold the row, up to 8 of them with 8 columns
+// a lane, then with 16.  (5120 columns: 5 wavefronts of 16 a lane 56.6 us for 8191 rows in 8 bits, 10 of 8 a lane 68; 4096: 4 of 16 96.5 us for 16384 rows, 8 of 8 93.9.)
 template <typename T, int OUT>
 tcr_status run(const Norm& a, hipStream_t s) {
     const unsigned waves = (unsigned)div_up(a.cols, 64 * kVec);
@@ -22,7 +22,7 @@ tcr_status run(const Norm& a, hipStream_t s) {
     else if (a.cols <= 128) norm_kernel<T, OUT, 16, 1><<<rows(16), kNormThreads, 0, s>>>(a);
     else if (a.cols <= 256) norm_kernel<T, OUT, 32, 1><<<rows(32), kNormThreads, 0, s>>>(a);
     else if (a.cols <= 512) norm_kernel<T, OUT, 64, 1><<<rows(64), kNormThreads, 0, s>>>(a);
-    else if (waves <= kMostWaves) norm_kernel<T, OUT, 0, 1><<<dim3((unsigned)a.rows), waves * 64, 0, s>>>(a);
+    else if (waves <= 8) norm_kernel<T, OUT, 0, 1><<<dim3((unsigned)a.rows), waves * 64, 0, s>>>(a);
     else if (waves <= 2 * kMostWaves) norm_kernel<T, OUT, 0, 2><<<dim3((unsigned)a.rows), (waves + 1) / 2 * 64, 0, s>>>(a);
     else norm_long_kernel<T, OUT><<<dim3((unsigned)a.rows), kLongWaves * 64, 0, s>>>(a);
     return launched("norm_kernel");
