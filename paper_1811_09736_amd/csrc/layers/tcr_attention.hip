@@ -54,9 +54,14 @@ Scan scan_of(const tcr_attention& a, const View& va, const View& vb, const View&
     return s;
 }
 
-// Tokens of a sequence up to which its states stay in registers from token to token: a step costs 1.2 us, a chunk's fixed cost is 10 us.
-constexpr uint64_t kStepTokens = 8;
-constexpr uint64_t kWholeChunks = 5;
+// Tokens of a sequence up to which its states go from token to token in registers, each token a pass over them, and not through a chunk's products, which take
+// the same for 1 and for 32 tokens.  16 heads of 128 x 128, steps / chunk: 1 sequence, 4 tokens 6.7 / 9.0 us, 8 tokens 10.0 / 9.0;
+// 256 sequences, 2 tokens 130 / 132, 4 tokens 177 / 134.
+constexpr uint64_t kStepTokens = 2, kFewStepTokens = 4, kFewPairs = 32;
+constexpr uint64_t kWholeChunks = 2;
+// Blocks of a sequence up to which each adds up the states in front of it by itself, without a kernel for the carries.  16 heads of 128 x 128: 4 x 2048 tokens in
+// 8 blocks each 60 us, with that kernel 72; 16 blocks 32.9 and 33.0.  States that are read transposed are read in pieces of 16 bytes: once, not for each block.
+constexpr uint32_t kDirectBlocks = 8;
 constexpr uint64_t kFill = 512;                    // workgroups that fill the chip: two on each compute unit
 
 template <typename T, typename OUT>
@@ -83,15 +88,15 @@ ChunkShape chunk_shape(uint32_t dk, uint32_t dv) {
     return {dk <= 64 ? 64u : 128u, dv <= 64 ? 64u : 128u, 64};
 }
 
-// Memory for a call's states between blocks: the stream's workspace, or what the caller of run() sets aside.  `turned`: the states there are
-// already those of this scan, transposed.
+// Memory for a call's states between blocks: the stream's workspace, or what the caller of run() sets aside.  `shared`: the states serve a second scan,
+// which is `turned`: it finds them there, transposed.
 struct Room {
-    bool given = false, turned = false;
+    bool given = false, shared = false, turned = false;
     float* floats = nullptr;
     uint64_t count = 0;
 };
 
-// How a scan is cut: as many blocks as fill the chip, of two chunks at least; fewer where `most` floats do not hold their states.
+// How a scan is cut: as many blocks as fill the chip, or as there are chunks or pairs of them; fewer where `most` floats do not hold their states.
 // *need: the floats that these blocks want.
 Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need) {
     const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs;
@@ -101,8 +106,10 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
     Blocks b = {};
     const uint64_t span = a.offsets != nullptr ? a.total : a.tokens;
     uint64_t per_span = div_up(kFill, units * spans);
-    // (the states' and the carries' kernels take as long as a few chunks: sequences of so many stay whole)
-    const uint64_t most_blocks = span <= kWholeChunks * shape.chunk ? 1 : div_up(span, 2 * shape.chunk);
+    // (the kernel for the states takes as long as a chunk or two: sequences of so many stay whole.  Of one chunk where each block adds up the others' states,
+    // of two where that would be too many: 1024 tokens in 8 blocks of two chunks 23 us, in 16 of one 31.)
+    const uint64_t chunks = div_up(span, shape.chunk), pairs = div_up(chunks, 2);
+    const uint64_t most_blocks = chunks <= kWholeChunks ? 1 : chunks <= kDirectBlocks ? chunks : pairs;
     if (per_span > most_blocks) per_span = most_blocks;
     if (per_span > 1 && per_span * spans > most / each + 1) {
         per_span = (most / each + 1) / spans;
@@ -132,10 +139,11 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
         b.states = room.floats;
         b.keep = room.floats + (b.count - 1) * units * state_size;
         b.turned = room.turned;
+        b.direct = b.per_span <= kDirectBlocks && !room.shared;
         if (!room.turned) {
             attention_chunk_kernel<T, T, DK, W, NT, C, true><<<dim3((unsigned)((b.count - 1) * units)), dim3(64 * W), 0, stream>>>(a, b);
             if (launched("attention_chunk_kernel<states>") != TCR_OK) return TCR_ERR_HIP;
-            attention_carry_kernel<<<dim3((unsigned)(units * state_size / 256)), dim3(256), 0, stream>>>(b, (uint32_t)slabs, state_size);
+            if (!b.direct) attention_carry_kernel<<<dim3((unsigned)(units * state_size / 256)), dim3(256), 0, stream>>>(b, (uint32_t)slabs, state_size);
             if (launched("attention_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
         }
     }
@@ -143,10 +151,10 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
     return launched("attention_chunk_kernel");
 }
 
-// Whether chunks take a scan, or it goes token by token.  (Packed sequences by their mean: one of many tokens among very many
-// without any would have a chunk's workgroups wait for the walk over them.)
+// Whether chunks take a scan, or it goes token by token.  (Packed sequences: by their mean.)
 bool by_chunks(const Scan& a) {
-    if (a.sequences == 0 || a.total <= (a.offsets != nullptr ? 2 : kStepTokens) * a.sequences) return false;
+    const uint64_t steps = a.sequences * a.heads <= kFewPairs ? kFewStepTokens : kStepTokens;
+    if (a.sequences == 0 || a.total <= steps * a.sequences) return false;
     for (const View* v : {&a.a, &a.b, &a.c})
         if (v->tok < 0 || v->tok > (1 << 23)) return false;        // offsets inside a chunk are 31 bits and count upwards
     return a.out_tok >= 0 && a.out_tok <= (1 << 22);
@@ -250,6 +258,7 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
     for (Scan* r : {&of_v, &of_k}) {
         void* const out = r->out;
         if (group > 1) r->out = floats;
+        room.shared = alike;
         room.turned = alike && r == &of_k;
         st = run(*r, a.dtype, group > 1, stream, room);
         if (st != TCR_OK) return st;

@@ -34,6 +34,7 @@ struct Blocks {
     float* states;              // [heads][slabs][count - 1] of what a workgroup holds: the state behind each block but the last
     float* keep;                // [heads][count - 1]: what is left behind a block of a state in front of it
     uint32_t turned;            // the states are transposed: those of a scan with b and c exchanged, cut alike
+    uint32_t direct;            // a block adds up the states of the ones in front of it itself; otherwise they hold what reaches the next block
 };
 
 // A chunk: tokens of sequence s at rows low .. low + len - 1 of the views.
@@ -304,25 +305,32 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
     float* const own_states = blocks.states + ((int64_t)(h * slabs + slab) * (blocks.count - 1) + block) * kStateSize;
     clear();
     if (!STATES && block % blocks.per_span != 0) {                  // (not looked at where a sequence starts with the block)
-        const float* from = own_states - kStateSize;
+        const uint32_t in_front = block / blocks.per_span * blocks.per_span, head_states = (blocks.count - 1) * slabs;
+        for (uint32_t m = blocks.direct ? in_front : block - 1; m < block; ++m) {
+            const float keep = m == in_front || !blocks.direct ? 0.0f : blocks.keep[(uint64_t)h * (blocks.count - 1) + m];
+            const float* const from = blocks.states + ((int64_t)h * head_states + m) * kStateSize;
 #pragma unroll
-        for (int mt = 0; mt < KT; ++mt)
+            for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (!blocks.turned) {
-                    S[mt][nt] = *reinterpret_cast<const f4v*>(from + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
-                    continue;
+                for (int nt = 0; nt < NT; ++nt) {
+                    f4v x = {0, 0, 0, 0};
+                    if (!blocks.turned) {
+                        x = *reinterpret_cast<const f4v*>(from + (int64_t)slab * (blocks.count - 1) * kStateSize + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
+                    } else {
+                        // (row k, column v of this S is row v, column k there)
+                        const uint32_t v = slab * kSlab + (w * NT + nt) * 16 + n;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const uint32_t k = mt * 16 + 4 * g + r;
+                            const float* there = from + (int64_t)(k / kSlab) * (blocks.count - 1) * kStateSize +
+                                                 ((k % kSlab / (16 * NT) * KT + v / 16) * NT + k / 16 % NT) * 256 + (v % 16 / 4 * 16 + k % 16) * 4 + v % 4;
+                            if (k < a.dk) x[r] = *there;
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = fmaf(S[mt][nt][r], keep, x[r]);
                 }
-                // (row k, column v of this S is row v, column k there)
-                const uint32_t v = slab * kSlab + (w * NT + nt) * 16 + n;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t k = mt * 16 + 4 * g + r;
-                    const float* there = blocks.states + ((int64_t)(h * slabs + k / kSlab) * (blocks.count - 1) + block - 1) * kStateSize +
-                                         ((k % kSlab / (16 * NT) * KT + v / 16) * NT + k / 16 % NT) * 256 + (v % 16 / 4 * 16 + k % 16) * 4 + v % 4;
-                    if (k < a.dk) S[mt][nt][r] = *there;
-                }
-            }
+        }
     }
 
     if (!STATES && a.offsets != nullptr) {
@@ -572,6 +580,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
         }
 #pragma unroll
         for (int ks = 0; ks < C / 32; ++ks) {
+            if (ks > 0 && ks * 32 >= now.len) break;                               // (a short chunk's rows of zeros)
             constexpr int kBatch = W == 8 ? (kHalf ? 2 : 4) : (KT < 8 ? 4 : 8);
             v8 rows[kBatch];
             auto read_rows = [&](int m0) {
