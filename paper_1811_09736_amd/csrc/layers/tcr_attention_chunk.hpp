@@ -20,7 +20,8 @@
 //
 // Rounding.  The matrix cores take 16-bit operands.  a, b and c are theirs exactly; the derived ones would cost the results half of
 // their precision if they were rounded: scores and S as a factor are given as two parts (high + low, 2 products), decayed c, whose sums are the
-// binary32 states, as three bfloat16 or two binary16 parts.  binary16 holds neither large nor small values, so scores, S and c are
+// binary32 states, as three bfloat16 or two binary16 parts (two of either for gradients without one of the states: not FINE; the states are
+// factors only there, 16 bits of theirs count, and an eighth of all products is saved).  binary16 holds neither large nor small values, so scores, S and c are
 // brought near 2^14 by powers of two there.
 #pragma once
 #include "tcr_attention.hpp"
@@ -201,11 +202,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(uniform(p)), 0, 0x7fffffff, 0x00020000);
 }
 
-template <typename T, typename OUT, int DK, int W, int NT, int C, bool STATES>
+template <typename T, typename OUT, int DK, int W, int NT, int C, bool STATES, bool FINE>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W / 2))) void attention_chunk_kernel(const Scan a, const Blocks blocks) {
     typedef typename Bits<T>::v8 v8;
     constexpr bool kHalf = std::is_same<T, _Float16>::value;
-    constexpr int CT = C / 16, KT = DK / 16, kParts = kHalf ? 2 : 3, kSlab = 16 * W * NT, KS = C / 32;
+    constexpr int CT = C / 16, KT = DK / 16, kParts = FINE && !kHalf ? 3 : 2, kSlab = 16 * W * NT, KS = C / 32;
     constexpr int kChunkThreads = 64 * W;
     typedef typename std::conditional<STATES, ChunkLds<T, DK, kSlab, C>, ChunkLdsOut<T, DK, kSlab, C>>::type Lds;
     constexpr int SA = Lds::kStrideA, SB = Lds::kStrideB, SC = Lds::kStrideC, SP = Lds::kStrideP;
