@@ -88,12 +88,18 @@ struct Walk {
         hi = reverse ? total - from : to;
         return true;
     }
+    // Where to go on from a token of no sequence: in front of all of them, behind them (offsets that decrease leave others: one by one).
+    __device__ __forceinline__ uint32_t beyond() const {
+        const uint32_t token = reverse ? total - 1 - pos : pos, first = cut(0), last = cut(sequences);
+        if (token < first) return reverse || first >= end ? end : first;
+        if (token >= last) return !reverse || total - last >= end ? end : total - last;
+        return pos + 1;
+    }
     template <int C>
     __device__ __forceinline__ bool next(Chunk& c) {
         while (pos < end) {
             if (pos >= hi && !find()) {
-                ++pos;
-                hi = pos;
+                pos = hi = beyond();
                 continue;
             }
             uint32_t stop = end - pos < C ? end : pos + C;
@@ -179,7 +185,7 @@ __device__ __forceinline__ float reciprocal_power(float f) { return __builtin_bi
 template <typename T, int DK, int COLS, int C>
 struct ChunkLds {
     // (rows 16 bytes beyond a multiple of 128: reads of 8 or 16 bytes from 16 rows meet no bank twice; 32 bytes: reads of columns)
-    static constexpr int kStrideA = DK + 8, kStrideB = DK + 16, kStrideC = COLS + 16, kStrideP = C + 8;
+    static constexpr int kStrideA = DK + 8, kStrideB = DK + 16, kStrideC = COLS + 16, kStrideP = C + 16;
     alignas(16) T b[C * kStrideB];
     alignas(16) T c[C * kStrideC];
     float beyond[C];                         // (what a look-up of steps behind a short chunk's end meets, for rows of zeros)
@@ -329,7 +335,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
                         }
                     }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = fmaf(S[mt][nt][r], keep, x[r]);
+                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = keep != 0.0f ? fmaf(S[mt][nt][r], keep, x[r]) : x[r];       // (NaN ends with its sequence)
                 }
         }
     }
@@ -663,7 +669,7 @@ __global__ __launch_bounds__(256) void attention_carry_kernel(const Blocks block
 #pragma unroll
         for (uint32_t i = 0; i < kAtOnce; ++i)
             if (n0 + i < end) {
-                carry = fmaf(carry, keep[n0 + i], own[i]);
+                carry = keep[n0 + i] != 0.0f ? fmaf(carry, keep[n0 + i], own[i]) : own[i];       // (NaN ends with its sequence)
                 states[(n0 + i) * state_size] = carry;
             }
     }
