@@ -62,7 +62,9 @@ constexpr uint64_t kWholeChunks = 2;
 // Blocks of a sequence up to which each adds up the states in front of it by itself, without a kernel for the carries.  16 heads of 128 x 128: 4 x 2048 tokens in
 // 8 blocks each 60 us, with that kernel 72; 16 blocks 32.9 and 33.0.  States that are read transposed are read in pieces of 16 bytes: once, not for each block.
 constexpr uint32_t kDirectBlocks = 8;
-constexpr uint64_t kFill = 512;                    // workgroups that fill the chip: two on each compute unit
+// Wavefronts that a launch is cut for: two on each SIMD, or four where blocks stay long, for whose states' bytes more of them make up.  16 heads of 128 x 128,
+// two / four: 4 x 2048 tokens, gradients, blocks of 512 / 256 tokens 172 / 186 us; 32768 tokens, blocks of 2048 / 1024 tokens 244 / 230 us.
+constexpr uint64_t kFillWaves = 2048, kLongChunks = 16;
 
 template <typename T, typename OUT>
 tcr_status run_steps(const Scan& a, hipStream_t stream) {
@@ -79,13 +81,13 @@ tcr_status run_steps(const Scan& a, hipStream_t stream) {
     return launched("attention_step_kernel");
 }
 
-// The kernel that takes a pair of widths: rows and columns of S that a workgroup holds, tokens of a chunk.
+// The kernel that takes a pair of widths: rows and columns of S that a workgroup holds, tokens of a chunk, wavefronts.
 struct ChunkShape {
-    uint32_t rows, cols, chunk;
+    uint32_t rows, cols, chunk, waves;
 };
 ChunkShape chunk_shape(uint32_t dk, uint32_t dv) {
-    if (dk > 128) return {256, 64, 32};
-    return {dk <= 64 ? 64u : 128u, dv <= 64 ? 64u : 128u, 64};
+    if (dk > 128) return {256, 64, 32, 4};
+    return {dk <= 64 ? 64u : 128u, dv <= 64 ? 64u : 128u, 64, dv <= 64 ? 4u : 8u};
 }
 
 // Memory for a call's states between blocks: the stream's workspace, or what the caller of run() sets aside.  `shared`: the states serve a second scan,
@@ -105,10 +107,11 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
     const uint64_t each = units * shape.rows * shape.cols + a.heads;
     Blocks b = {};
     const uint64_t span = a.offsets != nullptr ? a.total : a.tokens;
-    uint64_t per_span = div_up(kFill, units * spans);
+    const uint64_t chunks = div_up(span, shape.chunk), pairs = div_up(chunks, 2);
+    uint64_t per_span = div_up(2 * kFillWaves / shape.waves, units * spans);
+    if (chunks < per_span * kLongChunks) per_span = div_up(kFillWaves / shape.waves, units * spans);
     // (the kernel for the states takes as long as a chunk or two: sequences of so many stay whole.  Of one chunk where each block adds up the others' states,
     // of two where that would be too many: 1024 tokens in 8 blocks of two chunks 23 us, in 16 of one 31.)
-    const uint64_t chunks = div_up(span, shape.chunk), pairs = div_up(chunks, 2);
     const uint64_t most_blocks = chunks <= kWholeChunks ? 1 : chunks <= kDirectBlocks ? chunks : pairs;
     if (per_span > most_blocks) per_span = most_blocks;
     if (per_span > 1 && per_span * spans > most / each + 1) {
@@ -125,7 +128,7 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
 
 template <typename T, typename OUT, int DK, int W, int NT, int C, bool FINE>
 tcr_status run_chunks_as(const Scan& a, const Room& given, hipStream_t stream) {
-    const ChunkShape shape = {DK, 16 * W * NT, C};
+    const ChunkShape shape = {DK, 16 * W * NT, C, W};
     Room room = given;
     uint64_t need = 0;
     Blocks b = cut(a, shape, given.given ? given.count : ~0ull, &need);

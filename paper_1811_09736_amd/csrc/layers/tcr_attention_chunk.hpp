@@ -316,6 +316,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
         for (uint32_t m = blocks.direct ? in_front : block - 1; m < block; ++m) {
             const float keep = m == in_front || !blocks.direct ? 0.0f : blocks.keep[(uint64_t)h * (blocks.count - 1) + m];
             const float* const from = blocks.states + ((int64_t)h * head_states + m) * kStateSize;
+            if (keep == 0.0f) clear();                              // (NaN ends with its sequence)
 #pragma unroll
             for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
                         }
                     }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = keep != 0.0f ? fmaf(S[mt][nt][r], keep, x[r]) : x[r];       // (NaN ends with its sequence)
+                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = fmaf(S[mt][nt][r], keep, x[r]);
                 }
         }
     }
