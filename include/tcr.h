@@ -226,6 +226,9 @@ tcr_status tcr_scan(const void *in, float *out, uint64_t n, void *stream);
  * dk and dv: multiples of 8 from 8 to 256; fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED otherwise).  The magnitude of
  * scale lies between 1e-18 and 1e18.  As everywhere, inputs are finite: an infinity or NaN poisons its own sequence, also up to
  * 63 tokens in front of it.
+ * Results are the same from run to run.  Workspace: where sequences and heads are too few to fill the chip, tokens are cut into blocks whose states (dk x dv floats,
+ * rounded up to 64, 128 or 256, for each block and head) pass through it, 32 MiB as a rule and 64 MiB at most; with less of it, or none (a caller's buffer, a
+ * stream that is being recorded), the call takes fewer blocks and longer, and its sums other roundings.
  */
 typedef enum {
     TCR_F16 = 0,               /* IEEE binary16 */
@@ -253,8 +256,8 @@ tcr_status tcr_linear_attention_step(const tcr_attention *shape, const void *q, 
  * Gradients of tcr_linear_attention.  dout is laid out by o_stride; dq, dk, dv are contiguous (sequence, token, head, element
  * -- packed: token, head, element), dk and dv summed over the heads that share them.  state: the forward call's;
  * dfinal: the gradient of its final_state (NULL: none); dstate: the gradient of `state` (NULL: not wanted), not dfinal's array.
- * The decays are constants of a model and have no gradient here.  Where heads share keys and values the call needs tokens *
- * heads * max(dk, dv) floats of workspace.
+ * The decays are constants of a model and have no gradient here.  Where heads share keys and values the call needs tokens in all *
+ * heads * max(dk, dv) floats of workspace, in front of the states' (TCR_ERR_WORKSPACE where a caller's buffer, or what exists while a stream is recorded, is smaller).
  */
 tcr_status tcr_linear_attention_backward(const tcr_attention *shape, const void *dout, const void *q, const void *k, const void *v, void *dq, void *dk,
                                          void *dv, const float *state, const float *dfinal, float *dstate, void *stream);
@@ -282,8 +285,8 @@ tcr_status tcr_rms_norm_quantized(const void *x, const void *residual, const voi
 /*
  * Gradients of tcr_rms_norm from its `total` (x, where nothing was added) and rstd; dtotal: the gradient of `total`
  * itself, added to dx (NULL: none).  dx: rows x cols, contiguous, the gradient of x and of residual alike; dweight: cols elements
- * of the type of weight, the sum over all rows (the same from run to run).  Needs at most 1024 * cols floats of workspace and
- * runs with cols of them.
+ * of the type of weight, the sum over all rows (the same from run to run).  Takes at most 1024 * cols floats of workspace and
+ * runs with cols of them (TCR_ERR_WORKSPACE with less).
  */
 tcr_status tcr_rms_norm_backward(const void *dout, const void *total, const void *weight, const float *rstd, const void *dtotal, void *dx,
                                  void *dweight, uint64_t rows, uint64_t cols, int64_t dout_stride, int64_t total_stride, int64_t dtotal_stride,

@@ -1,6 +1,6 @@
 // binding.py's calls of linear attention and of the root-mean-square norm in their ordinary form (part of tcr_native.cpp, whose rules hold here: a
 // function returns None, before it has done anything, where binding.py has to look itself).  us a call, through Python / native, at sizes whose
-// kernels take less: a step of attention 16 / 6.5, a norm in 8 bits 15 / 5.5.
+// kernels take less: a step of attention 16 / 5.1, a norm in 8 bits 15 / 6.8.
 #pragma once
 
 decltype(&tcr_linear_attention) g_linear_attention;

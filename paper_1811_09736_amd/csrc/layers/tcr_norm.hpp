@@ -299,7 +299,8 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a
 }
 
 // Gradients: a row per wavefront and four per workgroup (LANES == 64), or a row per workgroup (0); each takes every parts-th of them, the next
-// row's loads on their way meanwhile, and keeps its sums of dweight in registers.
+// row's loads on their way meanwhile, and keeps its sums of dweight in registers.  MI355X: 16384 x 4096 bfloat16, 537 MB, in 99 us and 5 for the parts, 5.1 TB/s
+// (166 without the loads ahead, with four wavefronts of 16 columns a lane).
 template <typename T, int LANES, int ITEMS>
 __global__ __launch_bounds__(LANES == 0 ? kMostWaves * 64 : kNormThreads) void norm_grad_kernel(const NormGrad a) {
     static_assert(LANES == 0 || LANES == 64, "");
