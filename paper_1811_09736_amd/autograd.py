@@ -1,7 +1,9 @@
-"""Linear attention with decay and the root-mean-square norm as differentiable functions: binding's calls and their gradients, nothing else."""
+"""Linear attention with decay and the root-mean-square norm as differentiable functions: binding's calls and their gradients, nothing else
+(gradients of the gradients are refused)."""
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -16,6 +18,7 @@ class _LinearAttention(torch.autograd.Function):
         return out, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dlast):
         q, k, v, log_decay, offsets, state = ctx.saved_tensors
         if dout is None:
@@ -46,6 +49,7 @@ class _RmsNorm(torch.autograd.Function):
         return (out, total) if ctx.added else out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dtotal=None):
         total, weight, rstd = ctx.saved_tensors
         dout = torch.zeros_like(total) if dout is None else dout.contiguous()

@@ -49,9 +49,11 @@ tcr_status forward(const Norm& a, uint32_t dtype, uint32_t weight_dtype, uint32_
 
 template <typename T>
 tcr_status backward(NormGrad a, hipStream_t s) {
-    // as many parts as keep the chip busy, 16 wavefronts on each compute unit, or as there is room for
-    const unsigned waves = (unsigned)div_up(a.cols, 64 * kVec), items = waves <= kMostWaves ? 1 : 2, block = (waves + items - 1) / items * 64;
-    const uint64_t rows_at_once = waves == 1 ? kNormThreads / 64 : 1, units = div_up(a.rows, rows_at_once), held = waves <= 2 * kMostWaves ? div_up(4096, waves) : 1024;
+    // Rows of up to 1024 columns a wavefront each, four a workgroup, without barriers (32768 x 1024: 61 us, two wavefronts a row 71); up to 4096 columns 8 a lane with
+    // the next row's loads ahead (16384 x 4096: 102 us, 16 a lane without 108); then 16 a lane (8191 x 5120: 79 us, 8 a lane 99).
+    // As many parts as keep the chip busy, 16 wavefronts on each compute unit (twice as many: 5 to 10 % slower), or as there is room for.
+    const unsigned waves = (unsigned)div_up(a.cols, 64 * kVec), items = waves <= 8 && waves != 2 ? 1 : 2, block = (waves + items - 1) / items * 64;
+    const uint64_t rows_at_once = waves <= 2 ? kNormThreads / 64 : 1, units = div_up(a.rows, rows_at_once), held = waves <= 2 * kMostWaves ? div_up(4096, waves) : 1024;
     uint64_t parts = held > 1024 ? 1024 : (held < 256 ? 256 : held), got = 0;
     if (parts > units) parts = units != 0 ? units : 1;
     const tcr_status st = partials_for(s, parts * a.cols, &a.part, &got);
@@ -61,6 +63,7 @@ tcr_status backward(NormGrad a, hipStream_t s) {
     a.parts = (uint32_t)parts;
     const dim3 grid((unsigned)parts);
     if (waves == 1) norm_grad_kernel<T, 64, 1><<<grid, kNormThreads, 0, s>>>(a);
+    else if (waves == 2) norm_grad_kernel<T, 64, 2><<<grid, kNormThreads, 0, s>>>(a);
     else if (items == 1) norm_grad_kernel<T, 0, 1><<<grid, block, 0, s>>>(a);
     else if (waves <= 2 * kMostWaves) norm_grad_kernel<T, 0, 2><<<grid, block, 0, s>>>(a);
     else {

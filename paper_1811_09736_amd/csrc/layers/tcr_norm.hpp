@@ -321,7 +321,7 @@ __global__ __launch_bounds__(LANES == 0 ? kMostWaves * 64 : kNormThreads) void n
             if (a.dtotal != nullptr) more[i] = load_raw(static_cast<const T*>(a.dtotal) + (int64_t)row * a.dtotal_stride, col, cols);
         }
     };
-    constexpr bool kAhead = ITEMS == 1;                   // (two vectors a lane leave no registers for the next row's)
+    constexpr bool kAhead = ITEMS == 1 || LANES == 64;    // (two vectors a lane leave no registers for the next row's in a workgroup of 16 wavefronts)
     const uint64_t step = (uint64_t)a.parts * kRowsAtOnce;
     uint64_t row = (uint64_t)blockIdx.x * kRowsAtOnce + in_group;
     if (kAhead && row < a.rows) load(row);
