@@ -276,7 +276,7 @@ tcr_status tcr_rms_norm(const void *x, const void *residual, const void *weight,
 /*
  * The same with out in 8 bits: codes (rows x cols bytes, code_type TCR_E4M3 or TCR_I8) and one scale for each `group` columns of
  * a row (32, 64 or 128, the last group may be shorter; 0: one for the row), scales: rows x ceil(cols / group) floats.
- *   scale = max|out| / 448 (TCR_I8: 127), at least 2^-126;   code = out / scale, rounded to nearest even.
+ *   scale = max|out| / 448 (TCR_I8: 127), at least 2^-126;   code = out / scale, the binary32 quotient of both rounded to nearest even.
  * A row with an infinity or NaN has scales and codes that say so (codes of TCR_I8 are 0 there).
  */
 tcr_status tcr_rms_norm_quantized(const void *x, const void *residual, const void *weight, void *codes, float *scales, void *total, uint64_t rows,
