@@ -126,8 +126,8 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
     return b;
 }
 
-template <typename T, typename OUT, int DK, int W, int NT, int C, bool FINE>
-tcr_status run_chunks_as(const Scan& a, const Room& given, hipStream_t stream) {
+template <typename T, typename OUT, int DK, int W, int NT, int C>
+tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
     const ChunkShape shape = {DK, 16 * W * NT, C, W};
     Room room = given;
     uint64_t need = 0;
@@ -144,22 +144,14 @@ tcr_status run_chunks_as(const Scan& a, const Room& given, hipStream_t stream) {
         b.turned = room.turned;
         b.direct = b.per_span <= kDirectBlocks && !room.shared;
         if (!room.turned) {
-            attention_chunk_kernel<T, T, DK, W, NT, C, true, FINE><<<dim3((unsigned)((b.count - 1) * units)), dim3(64 * W), 0, stream>>>(a, b);
+            attention_chunk_kernel<T, T, DK, W, NT, C, true><<<dim3((unsigned)((b.count - 1) * units)), dim3(64 * W), 0, stream>>>(a, b);
             if (launched("attention_chunk_kernel<states>") != TCR_OK) return TCR_ERR_HIP;
             if (!b.direct) attention_carry_kernel<<<dim3((unsigned)(units * state_size / 256)), dim3(256), 0, stream>>>(b, (uint32_t)slabs, state_size);
             if (launched("attention_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
         }
     }
-    attention_chunk_kernel<T, OUT, DK, W, NT, C, false, FINE><<<dim3((unsigned)(b.count * units)), dim3(64 * W), 0, stream>>>(a, b);
+    attention_chunk_kernel<T, OUT, DK, W, NT, C, false><<<dim3((unsigned)(b.count * units)), dim3(64 * W), 0, stream>>>(a, b);
     return launched("attention_chunk_kernel");
-}
-
-// (binary16 has one form: two parts hold 22 bits of theirs)
-template <typename T, typename OUT, int DK, int W, int NT, int C>
-tcr_status run_chunks(const Scan& a, const Room& room, hipStream_t stream) {
-    if constexpr (!std::is_same<T, _Float16>::value)
-        if (!a.coarse) return run_chunks_as<T, OUT, DK, W, NT, C, true>(a, room, stream);
-    return run_chunks_as<T, OUT, DK, W, NT, C, false>(a, room, stream);
 }
 
 // Whether chunks take a scan, or it goes token by token.  (Packed sequences: by their mean.)
@@ -230,7 +222,6 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
     s.init = state;
     s.st_row = 1;
     s.st_col = a.dv;
-    s.coarse = 1;
     st = run(s, a.dtype, false, stream);
     if (st != TCR_OK) return st;
 
@@ -242,7 +233,6 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
         r.init = dfinal;
         r.init_mul = 1.0f / a.scale;
         r.fin_mul = a.scale;
-        r.coarse = dstate == nullptr;
         return r;
     };
     Scan of_k = reversed(vv, vo, vq, a.dv, a.dk, dk), of_v = reversed(vk, vq, vo, a.dk, a.dv, dv);

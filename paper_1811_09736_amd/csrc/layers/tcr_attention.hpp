@@ -36,7 +36,6 @@ struct Scan {
     float out_scale, init_mul, fin_mul;
     uint32_t heads, dk, dv;
     uint32_t reverse, late;
-    uint32_t coarse;            // the states are not results but factors of 16-bit results only: 16 bits of what is added to them are enough
 };
 
 // The natural logarithm of a head's decay; minus infinity (nothing is kept) as a number whose product with 0 is 0.

@@ -24,10 +24,10 @@
 //             the same order (4g .. 4g+3 and 16 + 4g .. 16 + 4g+3 of 32): reads of columns then meet no bank twice.
 //
 // Rounding.  The matrix cores take 16-bit operands.  a, b and c are theirs exactly; the derived ones would cost the results half of
-// their precision if they were rounded: scores and S as a factor are given as two parts (high + low, 2 products), decayed c, whose sums are the
-// binary32 states, as three bfloat16 or two binary16 parts (two of either for gradients without one of the states: not FINE; the states are
-// factors only there, 16 bits of theirs count, and an eighth of all products is saved).  binary16 holds neither large nor small values, so scores, S and c are
-// brought near 2^14 by powers of two there.
+// their precision if they were rounded: scores and S as a factor are given as two parts (high + low, 2 products, off by 2^-17 of themselves in bfloat16 and
+// 2^-20 in binary16, for outputs that are rounded by 2^-9 and 2^-12), decayed c, whose sums are the binary32 states, as three bfloat16 or two binary16 parts (2^-21 at most).
+// The gradients' states too, so that a gradient is the same whether the states' own is asked for or not (two bfloat16 parts for them: gradients of 4 x 2048 tokens, 16 heads of 128 x 128, 170 us instead of 181).
+// binary16 holds neither large nor small values, so scores, S and c are brought near 2^14 by powers of two there.
 #pragma once
 #include "tcr_attention.hpp"
 
@@ -213,11 +213,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(uniform(p)), 0, 0x7fffffff, 0x00020000);
 }
 
-template <typename T, typename OUT, int DK, int W, int NT, int C, bool STATES, bool FINE>
+template <typename T, typename OUT, int DK, int W, int NT, int C, bool STATES>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W / 2))) void attention_chunk_kernel(const Scan a, const Blocks blocks) {
     typedef typename Bits<T>::v8 v8;
     constexpr bool kHalf = std::is_same<T, _Float16>::value;
-    constexpr int CT = C / 16, KT = DK / 16, kParts = FINE && !kHalf ? 3 : 2, kSlab = 16 * W * NT, KS = C / 32;
+    constexpr int CT = C / 16, KT = DK / 16, kParts = kHalf ? 2 : 3, kSlab = 16 * W * NT, KS = C / 32;
     constexpr int kChunkThreads = 64 * W;
     typedef typename std::conditional<STATES, ChunkLds<T, DK, kSlab, C>, ChunkLdsOut<T, DK, kSlab, C>>::type Lds;
     constexpr int SA = Lds::kStrideA, SB = Lds::kStrideB, SC = Lds::kStrideC, SP = Lds::kStrideP;
