@@ -103,8 +103,8 @@ struct Room {
 Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need) {
     const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs;
     const uint64_t spans = a.offsets != nullptr ? 1 : a.sequences;
-    // (per block and unit a state, per block and head what is kept)
-    const uint64_t each = units * shape.rows * shape.cols + a.heads;
+    // (per block and unit a state, per block and head what is kept, two floats)
+    const uint64_t each = units * shape.rows * shape.cols + 2 * a.heads;
     Blocks b = {};
     const uint64_t span = a.offsets != nullptr ? a.total : a.tokens;
     const uint64_t chunks = div_up(span, shape.chunk), pairs = div_up(chunks, 2);
@@ -140,7 +140,7 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
     const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs, state_size = (uint64_t)DK * shape.cols;
     if (need != 0) {
         b.states = room.floats;
-        b.keep = room.floats + (b.count - 1) * units * state_size;
+        b.keep = reinterpret_cast<Kept*>(room.floats + (b.count - 1) * units * state_size);
         b.turned = room.turned;
         b.direct = b.per_span <= kDirectBlocks && !room.shared;
         if (!room.turned) {

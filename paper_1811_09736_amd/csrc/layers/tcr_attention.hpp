@@ -42,6 +42,28 @@ struct Scan {
 __device__ __forceinline__ float decay_of(const Scan& a, uint32_t h) { return fmaxf(a.log_decay[h], -1e30f); }
 // decay^steps
 __device__ __forceinline__ float decayed(float log_decay, float steps) { return expf(log_decay * steps); }
+// A state is multiplied by the same decay^steps chunk after chunk (token after token, block after block).  Near 1 the rounding of that one number, 2^-25, would add up over all
+// that the state remembers, to 2e-5 of it after 512 chunks; so where log_decay * steps lies within kNearOne, decay^steps - 1 is worked out too, by its series (whose
+// next term is 2^-29 of it there), and the sums below take what the rounding left out.
+constexpr float kNearOne = 0.25f;
+__device__ __forceinline__ bool near_one(float log_decay, float steps) { return fabsf(log_decay * steps) <= kNearOne; }
+__device__ __forceinline__ float less_one(float log_decay, float steps) {
+    const float x = log_decay * steps;
+    float sum = 1.0f;
+#pragma unroll
+    for (int i = 7; i >= 2; --i) sum = fmaf(sum * x, 1.0f / (float)i, 1.0f);
+    return sum * x;
+}
+// decay^steps as whole + rest, whole 1 or 0: S + (decay^steps - 1) S.
+struct Kept {
+    float whole, rest;
+};
+__device__ __forceinline__ Kept kept(float log_decay, float steps) {
+    return near_one(log_decay, steps) ? Kept{1.0f, less_one(log_decay, steps)} : Kept{0.0f, decayed(log_decay, steps)};
+}
+__device__ __forceinline__ bool nothing(const Kept& k) { return k.whole == 0.0f && k.rest == 0.0f; }
+// decay^steps x + y
+__device__ __forceinline__ float kept_plus(const Kept& k, float x, float y) { return fmaf(k.whole, x, fmaf(k.rest, x, y)); }
 
 // Tokens of sequence s: where they start and how many; whatever the offsets hold, inside [0, total).
 struct Span {
@@ -78,10 +100,7 @@ __global__ __launch_bounds__(kStepThreads) void attention_step_kernel(const Scan
     const bool live = col < a.dv;
     const Span span = span_of(a, s);
     const float log_decay = decay_of(a, h), lambda = decayed(log_decay, 1.0f);
-    // lambda S as S + (lambda - 1) S where lambda is near 1: lambda's own rounding, the same in every step, would add up over
-    // 1 / (1 - lambda) tokens (6e-5 of the state at lambda = 0.999)
-    const bool slow = lambda > 0.5f;
-    const float whole = slow ? 1.0f : 0.0f, rest = slow ? expm1f(log_decay) : lambda;
+    const Kept decay = kept(log_decay, 1.0f);
     const int64_t state = ((int64_t)s * a.heads + h) * a.dk * a.dv;
 
     f4v acc[kPasses];
@@ -106,8 +125,7 @@ __global__ __launch_bounds__(kStepThreads) void attention_step_kernel(const Scan
 
     for (uint64_t i = 0; i < span.count; ++i) {
         const int64_t t = a.reverse ? (int64_t)(span.count - 1 - i) : (int64_t)i;
-        const bool undecayed = a.late && i == 0;
-        const float e = undecayed ? 1.0f : whole, m = undecayed ? 0.0f : rest;
+        const Kept now = a.late && i == 0 ? Kept{1.0f, 0.0f} : decay;
         f4v c = {0, 0, 0, 0}, o = {0, 0, 0, 0};
         if (live)
             for (int j = 0; j < 4; ++j) c[j] = (float)pc[t * a.c.tok + col + j];
@@ -118,7 +136,7 @@ __global__ __launch_bounds__(kStepThreads) void attention_step_kernel(const Scan
                 const float b = (float)pb[t * a.b.tok + row], q = (float)pa[t * a.a.tok + row];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    acc[p][j] = fmaf(e, acc[p][j], fmaf(m, acc[p][j], b * c[j]));
+                    acc[p][j] = kept_plus(now, acc[p][j], b * c[j]);
                     o[j] = fmaf(q, acc[p][j], o[j]);
                 }
             }

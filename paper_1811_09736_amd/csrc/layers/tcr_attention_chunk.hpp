@@ -38,7 +38,7 @@ namespace layers {
 struct Blocks {
     uint32_t span, length, per_span, count;
     float* states;              // [heads][slabs][count - 1] of what a workgroup holds: the state behind each block but the last
-    float* keep;                // [heads][count - 1]: what is left behind a block of a state in front of it
+    Kept* keep;                 // [heads][count - 1]: what is left behind a block of a state in front of it (0: nothing reaches the next block)
     uint32_t turned;            // the states are transposed: those of a scan with b and c exchanged, cut alike
     uint32_t direct;            // a block adds up the states of the ones in front of it itself; otherwise they hold what reaches the next block
 };
@@ -52,6 +52,7 @@ struct Chunk {
 
 // (What is the same for a whole wavefront is kept in scalar registers, which the compiler has to be told of loaded values.)
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, uniform(__builtin_bit_cast(uint32_t, x))); }
 template <typename P>
 __device__ __forceinline__ P* uniform(P* p) {
     const uint64_t x = reinterpret_cast<uint64_t>(p);
@@ -195,6 +196,7 @@ struct ChunkLds {
     alignas(16) T c[C * kStrideC];
     float beyond[C];                         // (what a look-up of steps behind a short chunk's end meets, for rows of zeros)
     float powers[C + 1];                     // lambda^0 .. lambda^C
+    float missed[C + 1];                     // what their rounding left out, where lambda^C is near 1
 };
 template <typename T, int DK, int COLS, int C>
 struct ChunkLdsOut : ChunkLds<T, DK, COLS, C> {
@@ -256,12 +258,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
         const uint32_t from = some && walk.lo > block_start ? walk.lo : block_start;
         if (slab == 0 && threadIdx.x == 0)
             blocks.keep[(uint64_t)h * (blocks.count - 1) + block] =
-                some && walk.lo < block_start ? decayed(log_decay, (float)(walk.end - block_start)) : 0.0f;
+                some && walk.lo < block_start ? kept(log_decay, (float)(walk.end - block_start)) : Kept{0.0f, 0.0f};
         walk.pos = some ? from : walk.end;
     }
 
-    for (int i = threadIdx.x; i <= C; i += kChunkThreads) lds.powers[i] = decayed(log_decay, (float)i);
-    for (int i = threadIdx.x; i < C; i += kChunkThreads) lds.beyond[i] = 0.0f;
     const float* const powers = lds.beyond + C;                     // powers[-C .. C]
 
     // Rows of the next chunk on their way, 16 bytes a lane.  Rows and columns beyond the ends read as 0 (an offset outside the buffer).  A lane's
@@ -319,9 +319,9 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
     if (!STATES && block % blocks.per_span != 0) {                  // (not looked at where a sequence starts with the block)
         const uint32_t in_front = block / blocks.per_span * blocks.per_span, head_states = (blocks.count - 1) * slabs;
         for (uint32_t m = blocks.direct ? in_front : block - 1; m < block; ++m) {
-            const float keep = m == in_front || !blocks.direct ? 0.0f : blocks.keep[(uint64_t)h * (blocks.count - 1) + m];
+            const Kept keep = m == in_front || !blocks.direct ? Kept{0.0f, 0.0f} : blocks.keep[(uint64_t)h * (blocks.count - 1) + m];
             const float* const from = blocks.states + ((int64_t)h * head_states + m) * kStateSize;
-            if (keep == 0.0f) clear();                              // (NaN ends with its sequence)
+            if (nothing(keep)) clear();                             // (NaN ends with its sequence)
 #pragma unroll
             for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
                         }
                     }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = fmaf(S[mt][nt][r], keep, x[r]);
+                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = kept_plus(keep, S[mt][nt][r], x[r]);
                 }
         }
     }
@@ -368,10 +368,17 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
             }
     }
 
-    __syncthreads();
+    float missed = 0.0f;                                            // what the roundings of the state's decays have left out so far
     Chunk now, ahead;
     bool more = walk.next<C>(now);
     if (more) fetch_all(now);
+    // (while the rows are on their way; the chunk's first barrier stands in front of the first look-up)
+    for (int i = threadIdx.x; i <= C; i += kChunkThreads) {
+        const float power = decayed(log_decay, (float)i);
+        lds.powers[i] = power;
+        lds.missed[i] = near_one(log_decay, (float)C) ? less_one(log_decay, (float)i) - (power - 1.0f) : 0.0f;
+    }
+    for (int i = threadIdx.x; i < C; i += kChunkThreads) lds.beyond[i] = 0.0f;
     while (more) {
         // (addresses are worked out in every chunk: kept in registers all along they would push others to memory, and the wait for one of those
         // is a wait for the next chunk's rows too)
@@ -397,6 +404,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
         if (more) fetch_all(ahead);
 
         if (now.begin) {
+            missed = 0.0f;
             if (a.init != nullptr) {
                 const __amdgpu_buffer_rsrc_t from = buffer_at(a.init + ((int64_t)now.s * a.heads + h) * state_floats);
                 each([&](float, uint32_t at) { return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, 0)) * a.init_mul; });
@@ -584,61 +592,75 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
             // (values that two parts hold to 22 bits as they are stay as they are)
             if (!(largest_c >= 0.125f && largest_c < 32768.0f)) factor_c = near_top(largest_c);
         }
-        {
-            const float f = lds.powers[now.len - late] * factor_c;
+        // (what the chunk adds is summed apart and comes to S at once: one rounding of its size a chunk, and not one for each product.  The decay is rounded so
+        // that it makes up for what the roundings of the ones before it have left out: its own is the same in every chunk)
+        if (STATES || (now.last ? a.fin != nullptr : more)) {                      // (a state that nothing follows is not worked out)
+            const int steps = now.len - late;
+            const float power = lds.powers[steps], owed = lds.missed[steps] + missed, decay = power + owed;
+            missed = uniform(owed - (decay - power));
+            constexpr int kBatch = W == 8 ? 2 : 4;                                 // (as registers allow)
+            constexpr int kSteps = KT / kBatch * KS;
+            v8 rows[2][kBatch];                                                    // of these 32 tokens and kBatch * 16 rows of S, and the next on their way
+            auto read_rows = [&](int i) {
 #pragma unroll
-            for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) S[mt][nt] *= f;
-        }
-#pragma unroll
-        for (int ks = 0; ks < C / 32; ++ks) {
-            if (ks > 0 && ks * 32 >= now.len) break;                               // (a short chunk's rows of zeros)
-            constexpr int kBatch = W == 8 ? (kHalf ? 2 : 4) : (KT < 8 ? 4 : 8);
-            v8 rows[kBatch];
-            auto read_rows = [&](int m0) {
-#pragma unroll
-                for (int m = 0; m < kBatch; ++m)
-                    rows[m] = joined<T>(columns(lds.b, SB, ks * 32 + 4 * g, (m0 + m) * 16, n), columns(lds.b, SB, ks * 32 + 16 + 4 * g, (m0 + m) * 16, n));
+                for (int m = 0; m < kBatch; ++m) {
+                    const int from = i % KS * 32 + 4 * g, at = (i / KS * kBatch + m) * 16;
+                    rows[i & 1][m] = joined<T>(columns(lds.b, SB, from, at, n), columns(lds.b, SB, from + 16, at, n));
+                }
             };
-            u4v part[kParts][NT];
-            float decays[8];
+            u4v part[KS][kParts][NT];
+            if (W != 8) read_rows(0);
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                decays[r] = powers[now.len - 1 - (ks * 32 + (r >> 2) * 16 + 4 * g + (r & 3))];
-                if constexpr (kHalf) decays[r] *= factor_c;
+            for (int ks = 0; ks < KS; ++ks) {
+                float decays[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    decays[r] = powers[now.len - 1 - (ks * 32 + (r >> 2) * 16 + 4 * g + (r & 3))];
+                    if constexpr (kHalf) decays[r] *= factor_c;
+                }
+                loads_first();
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        uint32_t y[kParts];
+                        split<T, kParts>((float)cols[ks][nt][2 * r] * decays[2 * r], (float)cols[ks][nt][2 * r + 1] * decays[2 * r + 1], y, true);
+#pragma unroll
+                        for (int p = 0; p < kParts; ++p) part[ks][p][nt][r] = y[p];
+                    }
+                loads_first();
             }
-            read_rows(0);
-            loads_first();
+            if (W == 8) read_rows(0);
+            f4v add[kBatch][NT];
+            // (negated twice: an instruction with a negated operand keeps S in its place, without one the sum goes to the place of `add` and 32 registers do not fit)
+            const float minus = settled(-decay * factor_c);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    uint32_t y[kParts];
-                    split<T, kParts>((float)cols[ks][nt][2 * r] * decays[2 * r], (float)cols[ks][nt][2 * r + 1] * decays[2 * r + 1], y, true);
-#pragma unroll
-                    for (int p = 0; p < kParts; ++p) part[p][nt][r] = y[p];
-                }
-#pragma unroll
-            for (int m0 = 0; m0 < KT; m0 += kBatch) {
-                if (m0 > 0) {
-                    read_rows(m0);
-                    loads_first();
-                }
+            for (int i = 0; i < kSteps; ++i) {
+                const int ks = i % KS, m0 = i / KS * kBatch;
+                if (i + 1 < kSteps) read_rows(i + 1);
+                loads_first();
 #pragma unroll
                 for (int p = kParts - 1; p >= 0; --p)
 #pragma unroll
                     for (int m = 0; m < kBatch; ++m)
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) S[m0 + m][nt] = mfma(rows[m], __builtin_bit_cast(v8, part[p][nt]), S[m0 + m][nt]);
+                        for (int nt = 0; nt < NT; ++nt)
+                            add[m][nt] = mfma(rows[i & 1][m], __builtin_bit_cast(v8, part[ks][p][nt]), ks == 0 && p == kParts - 1 ? f4v{0, 0, 0, 0} : add[m][nt]);
+                if (ks == KS - 1)
+#pragma unroll
+                    for (int m = 0; m < kBatch; ++m)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) S[m0 + m][nt][r] = fmaf(-S[m0 + m][nt][r], minus, add[m][nt][r]);
             }
-        }
-        if (kHalf && factor_c != 1.0f) {
-            const float f = reciprocal_power(factor_c);
+            if (kHalf && factor_c != 1.0f) {
+                const float f = reciprocal_power(factor_c);
 #pragma unroll
-            for (int mt = 0; mt < KT; ++mt)
+                for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) S[mt][nt] *= f;
+                    for (int nt = 0; nt < NT; ++nt) S[mt][nt] *= f;
+            }
         }
         if (!STATES && now.last && a.fin != nullptr) {
             const __amdgpu_buffer_rsrc_t to = buffer_at(a.fin + ((int64_t)now.s * a.heads + h) * state_floats);
@@ -664,7 +686,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
 __global__ __launch_bounds__(256) void attention_carry_kernel(const Blocks blocks, uint32_t slabs, uint64_t state_size) {
     const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, group = at / state_size;      // (head, slab); state_size: a multiple of 256
     float* states = blocks.states + group * (blocks.count - 1) * state_size + at % state_size;
-    const float* keep = blocks.keep + group / slabs * (blocks.count - 1);
+    const Kept* keep = blocks.keep + group / slabs * (blocks.count - 1);
     float carry = 0.0f;
     constexpr uint32_t kAtOnce = 16;         // the loads of many blocks at once, then their sums
     const uint32_t end = blocks.count - 1;
@@ -675,7 +697,7 @@ __global__ __launch_bounds__(256) void attention_carry_kernel(const Blocks block
 #pragma unroll
         for (uint32_t i = 0; i < kAtOnce; ++i)
             if (n0 + i < end) {
-                carry = keep[n0 + i] != 0.0f ? fmaf(carry, keep[n0 + i], own[i]) : own[i];       // (NaN ends with its sequence)
+                carry = nothing(keep[n0 + i]) ? own[i] : kept_plus(keep[n0 + i], carry, own[i]);       // (NaN ends with its sequence)
                 states[(n0 + i) * state_size] = carry;
             }
     }
