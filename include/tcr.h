@@ -257,7 +257,9 @@ tcr_status tcr_linear_attention_step(const tcr_attention *shape, const void *q, 
  * -- packed: token, head, element), dk and dv summed over the heads that share them.  state: the forward call's;
  * dfinal: the gradient of its final_state (NULL: none); dstate: the gradient of `state` (NULL: not wanted), not dfinal's array.
  * The decays are constants of a model and have no gradient here.  Where heads share keys and values the call needs tokens in all *
- * heads * max(dk, dv) floats of workspace, in front of the states' (TCR_ERR_WORKSPACE where a caller's buffer, or what exists while a stream is recorded, is smaller).
+ * heads * max(dk, dv) floats of workspace, rounded up to a multiple of 64, in front of the states'.  Of a caller's buffer that is the second half of what follows its first
+ * 256 bytes: a buffer of 256 + 8 bytes for each of these floats (and up to 128 MiB for the states) is enough; with less the call returns TCR_ERR_WORKSPACE, and
+ * TCR_ERR_UNSUPPORTED where the stream is being recorded and its workspace is too small yet, and has done nothing.
  */
 tcr_status tcr_linear_attention_backward(const tcr_attention *shape, const void *dout, const void *q, const void *k, const void *v, void *dq, void *dk,
                                          void *dv, const float *state, const float *dfinal, float *dstate, void *stream);
@@ -286,7 +288,7 @@ tcr_status tcr_rms_norm_quantized(const void *x, const void *residual, const voi
  * Gradients of tcr_rms_norm from its `total` (x, where nothing was added) and rstd; dtotal: the gradient of `total`
  * itself, added to dx (NULL: none).  dx: rows x cols, contiguous, the gradient of x and of residual alike; dweight: cols elements
  * of the type of weight, the sum over all rows (the same from run to run).  Takes at most 1024 * cols floats of workspace and
- * runs with cols of them (TCR_ERR_WORKSPACE with less).
+ * runs with cols of them (with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, as above).
  */
 tcr_status tcr_rms_norm_backward(const void *dout, const void *total, const void *weight, const float *rstd, const void *dtotal, void *dx,
                                  void *dweight, uint64_t rows, uint64_t cols, int64_t dout_stride, int64_t total_stride, int64_t dtotal_stride,

@@ -133,7 +133,7 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
     uint64_t need = 0;
     Blocks b = cut(a, shape, given.given ? given.count : ~0ull, &need);
     if (need != 0 && !given.given) {
-        const tcr_status st = partials_for(stream, need, &room.floats, &room.count);
+        const tcr_status st = partials_for(stream, need, 0, &room.floats, &room.count);
         if (st != TCR_OK) return st;
         if (room.count < need) b = cut(a, shape, room.count, &need);
     }
@@ -222,8 +222,6 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
     s.init = state;
     s.st_row = 1;
     s.st_col = a.dv;
-    st = run(s, a.dtype, false, stream);
-    if (st != TCR_OK) return st;
 
     // dk and dv, from the last token to the first
     auto reversed = [&](const View& va, const View& vb, const View& vc, uint32_t rows, uint32_t cols, void* out) {
@@ -243,16 +241,22 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
     // Gradients of shared keys and values go by way of each head's own in binary32, in front of the states in the workspace.
     const uint64_t part = group == 1 ? 0 : div_up(of_k.total * a.heads * (a.dk > a.dv ? a.dk : a.dv), 64) * 64;
     const ChunkShape shape_k = chunk_shape(of_k.dk, of_k.dv), shape_v = chunk_shape(of_v.dk, of_v.dv);
-    uint64_t need_k = 0, need_v = 0, got = 0;
-    if (by_chunks(of_k)) (void)cut(of_k, shape_k, ~0ull, &need_k);
-    if (by_chunks(of_v)) (void)cut(of_v, shape_v, ~0ull, &need_v);
+    auto need_of = [](const Scan& r) {
+        uint64_t need = 0;
+        if (by_chunks(r)) (void)cut(r, chunk_shape(r.dk, r.dv), ~0ull, &need);
+        return need;
+    };
+    const uint64_t need_q = need_of(s), need_k = need_of(of_k), need_v = need_of(of_v);
+    const uint64_t behind = part + (need_k > need_v ? need_k : need_v);
+    // (all of it in front of the first launch: a call that lacks room has done nothing)
+    uint64_t got = 0;
     Room room;
     room.given = true;
-    if (part + (need_k > need_v ? need_k : need_v) != 0) {
-        st = partials_for(stream, part + (need_k > need_v ? need_k : need_v), &room.floats, &got);
-        if (st != TCR_OK) return st;
-        if (got < part) return TCR_ERR_WORKSPACE;
-    }
+    st = partials_for(stream, need_q > behind ? need_q : behind, part, &room.floats, &got);
+    if (st != TCR_OK) return st;
+    room.count = got;
+    st = run(s, a.dtype, false, stream, room);
+    if (st != TCR_OK) return st;
     float* const floats = room.floats;
     room.floats += part;
     room.count = got - part;

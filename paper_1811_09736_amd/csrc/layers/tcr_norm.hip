@@ -56,10 +56,9 @@ tcr_status backward(NormGrad a, hipStream_t s) {
     const uint64_t rows_at_once = waves <= 2 ? kNormThreads / 64 : 1, units = div_up(a.rows, rows_at_once), held = waves <= 2 * kMostWaves ? div_up(4096, waves) : 1024;
     uint64_t parts = held > 1024 ? 1024 : (held < 256 ? 256 : held), got = 0;
     if (parts > units) parts = units != 0 ? units : 1;
-    const tcr_status st = partials_for(s, parts * a.cols, &a.part, &got);
+    const tcr_status st = partials_for(s, parts * a.cols, a.cols, &a.part, &got);
     if (st != TCR_OK) return st;
     parts = got / a.cols;
-    if (parts == 0) return TCR_ERR_WORKSPACE;
     a.parts = (uint32_t)parts;
     const dim3 grid((unsigned)parts);
     if (waves == 1) norm_grad_kernel<T, 64, 1><<<grid, kNormThreads, 0, s>>>(a);

@@ -11,8 +11,9 @@ namespace host {
 
 // Room for `want` floats in the workspace that calls on `stream` use (a multiple of 256 bytes, aligned to 256 bytes), or for
 // fewer where it cannot be grown -- the caller's buffer, a stream that is being recorded: *got says how many, at most `want`.
-// The memory belongs to the calls on the stream in their order, as all of the workspace does.
-tcr_status partials_for(hipStream_t stream, uint64_t want, float** room, uint64_t* got);
+// The memory belongs to the calls on the stream in their order, as all of the workspace does.  With room for fewer than `least` the call cannot go on: what it
+// returns then (a caller's buffer: TCR_ERR_WORKSPACE, a stream that is being recorded: TCR_ERR_UNSUPPORTED).
+tcr_status partials_for(hipStream_t stream, uint64_t want, uint64_t least, float** room, uint64_t* got);
 
 // TCR_OK, or TCR_ERR_HIP with the error's text kept for tcr_last_hip_error.
 tcr_status launched(const char* what);

@@ -7,7 +7,7 @@ using namespace tcr;
 using namespace tcr::host;
 
 // ------------------------------------------------------------------------------ for the operators in layers/
-tcr_status tcr::host::partials_for(hipStream_t stream, uint64_t want, float** room, uint64_t* got) {
+tcr_status tcr::host::partials_for(hipStream_t stream, uint64_t want, uint64_t least, float** room, uint64_t* got) {
     *room = nullptr;
     *got = 0;
     if (want == 0) return TCR_OK;
@@ -16,6 +16,7 @@ tcr_status tcr::host::partials_for(hipStream_t stream, uint64_t want, float** ro
     tcr_status st = get_workspace(stream, &ws, &capturing);
     if (st != TCR_OK) return st;
     const uint64_t most = partials_limit(ws, capturing);
+    if (least > most) return ws->caller_owned ? TCR_ERR_WORKSPACE : TCR_ERR_UNSUPPORTED;
     if (want > most) want = most;
     if (want == 0) return TCR_OK;
     st = ensure_partials(ws, stream, want, capturing);
