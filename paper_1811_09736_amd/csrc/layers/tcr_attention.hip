@@ -66,16 +66,19 @@ constexpr uint32_t kDirectBlocks = 8;
 // two / four: 4 x 2048 tokens, gradients, blocks of 512 / 256 tokens 172 / 186 us; 32768 tokens, blocks of 2048 / 1024 tokens 244 / 230 us.
 constexpr uint64_t kFillWaves = 2048, kLongChunks = 16;
 
+// Workgroups for a kernel whose workgroups take the place of others behind the last.
+unsigned at_most(uint64_t blocks) { return (unsigned)(blocks < kGridRow ? blocks : kGridRow); }
+
 template <typename T, typename OUT>
 tcr_status run_steps(const Scan& a, hipStream_t stream) {
     if (a.offsets != nullptr && a.total != 0) {
-        attention_outside_kernel<OUT><<<dim3((unsigned)div_up(a.total, 64)), dim3(256), 0, stream>>>(a);
+        attention_outside_kernel<OUT><<<dim3(at_most(div_up(a.total, 64))), dim3(256), 0, stream>>>(a);
         if (launched("attention_outside_kernel") != TCR_OK) return TCR_ERR_HIP;
     }
     const uint64_t pairs = a.sequences * a.heads;
     if (pairs == 0) return TCR_OK;
     if (pairs * div_up(a.dv, 64) >= 1024)
-        attention_step_kernel<T, 16, OUT><<<dim3((unsigned)(pairs * div_up(a.dv, 64))), dim3(kStepThreads), 0, stream>>>(a);
+        attention_step_kernel<T, 16, OUT><<<grid_of(pairs * div_up(a.dv, 64)), dim3(kStepThreads), 0, stream>>>(a);
     else
         attention_step_kernel<T, 4, OUT><<<dim3((unsigned)(pairs * div_up(a.dv, 16))), dim3(kStepThreads), 0, stream>>>(a);
     return launched("attention_step_kernel");
@@ -150,7 +153,7 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
             if (launched("attention_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
         }
     }
-    attention_chunk_kernel<T, OUT, DK, W, NT, C, false><<<dim3((unsigned)(b.count * units)), dim3(64 * W), 0, stream>>>(a, b);
+    attention_chunk_kernel<T, OUT, DK, W, NT, C, false><<<grid_of(b.count * units), dim3(64 * W), 0, stream>>>(a, b);
     return launched("attention_chunk_kernel");
 }
 
@@ -271,7 +274,7 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
         if (st != TCR_OK) return st;
         const uint64_t count = r->total * a.kv_heads * r->dv;
         if (group == 1 || count == 0) continue;
-        const dim3 grid((unsigned)div_up(count, 256));
+        const dim3 grid(at_most(div_up(count, 256)));
         if (a.dtype == TCR_F16) attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(floats, static_cast<_Float16*>(out), count, r->dv, group);
         else attention_shared_kernel<<<grid, dim3(256), 0, stream>>>(floats, static_cast<__bf16*>(out), count, r->dv, group);
         if (launched("attention_shared_kernel") != TCR_OK) return TCR_ERR_HIP;

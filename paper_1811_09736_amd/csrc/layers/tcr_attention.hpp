@@ -93,12 +93,14 @@ __global__ __launch_bounds__(kStepThreads) void attention_step_kernel(const Scan
     constexpr int kRows = kStepThreads / LANES, kPasses = 256 / kRows, kWaves = kStepThreads / 64;
     __shared__ float sums[2][kWaves][4 * LANES];
     const uint32_t slabs = (a.dv + 4 * LANES - 1) / (4 * LANES);
-    const uint32_t slab = blockIdx.x % slabs, h = blockIdx.x / slabs % a.heads;
-    const uint64_t s = blockIdx.x / slabs / a.heads;
+    const uint32_t group = workgroup(), slab = group % slabs, h = group / slabs % a.heads;       // (fewer than 2^29 in all)
+    const bool there = group / slabs / a.heads < a.sequences;         // (or a workgroup that nothing is left for)
+    const uint64_t s = there ? group / slabs / a.heads : 0;
     const int lane = threadIdx.x % LANES, row0 = threadIdx.x / LANES, wave = threadIdx.x / 64;
     const uint32_t col = slab * 4 * LANES + lane * 4;
-    const bool live = col < a.dv;
-    const Span span = span_of(a, s);
+    const bool live = there && col < a.dv;
+    Span span = span_of(a, s);
+    if (!there) span.count = 0;
     const float log_decay = decay_of(a, h), lambda = decayed(log_decay, 1.0f);
     const Kept decay = kept(log_decay, 1.0f);
     const int64_t state = ((int64_t)s * a.heads + h) * a.dk * a.dv;
@@ -170,27 +172,28 @@ __global__ __launch_bounds__(kStepThreads) void attention_step_kernel(const Scan
     }
 }
 
-// Zeros in the rows of tokens that lie in no sequence.  One workgroup per 64 tokens.
+// Zeros in the rows of tokens that lie in no sequence.  One workgroup per 64 tokens, and every gridDim.x-th 64 behind them.
 template <typename OUT>
 __global__ __launch_bounds__(256) void attention_outside_kernel(const Scan a) {
     const uint64_t first = a.offsets[0], last = a.offsets[a.sequences];
-    for (uint64_t t = (uint64_t)blockIdx.x * 64; t < a.total && t < (uint64_t)blockIdx.x * 64 + 64; ++t) {
-        if (t >= first && t < last) continue;
-        OUT* out = static_cast<OUT*>(a.out) + (int64_t)t * a.out_tok;
-        for (uint32_t i = threadIdx.x; i < a.heads * a.dv; i += 256) out[(int64_t)(i / a.dv) * a.out_head + i % a.dv] = (OUT)0.0f;
-    }
+    for (uint64_t from = (uint64_t)blockIdx.x * 64; from < a.total; from += (uint64_t)gridDim.x * 64)
+        for (uint64_t t = from; t < a.total && t < from + 64; ++t) {
+            if (t >= first && t < last) continue;
+            OUT* out = static_cast<OUT*>(a.out) + (int64_t)t * a.out_tok;
+            for (uint32_t i = threadIdx.x; i < a.heads * a.dv; i += 256) out[(int64_t)(i / a.dv) * a.out_head + i % a.dv] = (OUT)0.0f;
+        }
 }
 
 // Gradients of shared keys and values: the sum over the heads that share them, in binary32, rounded once.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_shared_kernel(const float* __restrict__ part, T* __restrict__ out, uint64_t count, uint32_t d,
                                                                uint32_t group) {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;         // (token, shared head, column)
-    if (i >= count) return;
-    const float* from = part + i / d * group * d + i % d;
-    float sum = 0.0f;
-    for (uint32_t g = 0; g < group; ++g) sum += from[(uint64_t)g * d];
-    out[i] = (T)sum;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (uint64_t)gridDim.x * 256) {         // (token, shared head, column)
+        const float* from = part + i / d * group * d + i % d;
+        float sum = 0.0f;
+        for (uint32_t g = 0; g < group; ++g) sum += from[(uint64_t)g * d];
+        out[i] = (T)sum;
+    }
 }
 
 }  // namespace layers

@@ -228,7 +228,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
     const int w = (int)uniform(threadIdx.x >> 6);
     int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const uint32_t slabs = (a.dv + kSlab - 1) / kSlab;
-    const uint32_t slab = blockIdx.x % slabs, h = blockIdx.x / slabs % a.heads, block = blockIdx.x / slabs / a.heads;
+    const uint32_t group = workgroup(), slab = group % slabs, h = group / slabs % a.heads, block = group / slabs / a.heads;      // (fewer than 2^29 in all)
     const float log_decay = decay_of(a, h);
     constexpr int kHeld = KT * NT * 4;                              // floats of S a lane holds
     constexpr uint32_t kStateSize = kChunkThreads * kHeld;
@@ -250,6 +250,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
     const uint32_t block_start = span_first + in_span;
     walk.pos = block_start;
     walk.end = blocks.span - in_span < blocks.length ? span_first + blocks.span : block_start + blocks.length;
+    // (a workgroup that nothing is left for, which only whole sequences' grids have, finds no token; an exit up there would part the loads of the arguments: 0.4 us a launch)
+    if (block >= blocks.count) walk.end = block_start;
     walk.s = walk.lo = walk.hi = 0;
     if constexpr (STATES) {
         // only the sequence that goes on behind the block counts
@@ -368,17 +370,17 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
             }
     }
 
+    // (the chunk's first barrier stands in front of the first look-up)
+    if (threadIdx.x <= C) {
+        const float power = decayed(log_decay, (float)threadIdx.x);
+        lds.powers[threadIdx.x] = power;
+        lds.missed[threadIdx.x] = near_one(log_decay, (float)C) ? less_one(log_decay, (float)threadIdx.x) - (power - 1.0f) : 0.0f;
+        if (threadIdx.x < C) lds.beyond[threadIdx.x] = 0.0f;
+    }
     float missed = 0.0f;                                            // what the roundings of the state's decays have left out so far
     Chunk now, ahead;
     bool more = walk.next<C>(now);
     if (more) fetch_all(now);
-    // (while the rows are on their way; the chunk's first barrier stands in front of the first look-up)
-    for (int i = threadIdx.x; i <= C; i += kChunkThreads) {
-        const float power = decayed(log_decay, (float)i);
-        lds.powers[i] = power;
-        lds.missed[i] = near_one(log_decay, (float)C) ? less_one(log_decay, (float)i) - (power - 1.0f) : 0.0f;
-    }
-    for (int i = threadIdx.x; i < C; i += kChunkThreads) lds.beyond[i] = 0.0f;
     while (more) {
         // (addresses are worked out in every chunk: kept in registers all along they would push others to memory, and the wait for one of those
         // is a wait for the next chunk's rows too)

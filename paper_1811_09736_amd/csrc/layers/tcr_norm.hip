@@ -17,14 +17,14 @@ constexpr uint64_t kMostRows = 1ull << 31, kMostCols = 1ull << 24;
 template <typename T, int OUT>
 tcr_status run(const Norm& a, hipStream_t s) {
     const unsigned waves = (unsigned)div_up(a.cols, 64 * kVec);
-    auto rows = [&](unsigned lanes) { return dim3((unsigned)div_up(a.rows, kNormThreads / lanes)); };
+    auto rows = [&](unsigned lanes) { return grid_of(div_up(a.rows, kNormThreads / lanes)); };
     if (a.cols <= 64) norm_kernel<T, OUT, 8, 1><<<rows(8), kNormThreads, 0, s>>>(a);
     else if (a.cols <= 128) norm_kernel<T, OUT, 16, 1><<<rows(16), kNormThreads, 0, s>>>(a);
     else if (a.cols <= 256) norm_kernel<T, OUT, 32, 1><<<rows(32), kNormThreads, 0, s>>>(a);
     else if (a.cols <= 512) norm_kernel<T, OUT, 64, 1><<<rows(64), kNormThreads, 0, s>>>(a);
-    else if (waves <= 8) norm_kernel<T, OUT, 0, 1><<<dim3((unsigned)a.rows), waves * 64, 0, s>>>(a);
-    else if (waves <= 2 * kMostWaves) norm_kernel<T, OUT, 0, 2><<<dim3((unsigned)a.rows), (waves + 1) / 2 * 64, 0, s>>>(a);
-    else norm_long_kernel<T, OUT><<<dim3((unsigned)a.rows), kLongWaves * 64, 0, s>>>(a);
+    else if (waves <= 8) norm_kernel<T, OUT, 0, 1><<<grid_of(a.rows), waves * 64, 0, s>>>(a);
+    else if (waves <= 2 * kMostWaves) norm_kernel<T, OUT, 0, 2><<<grid_of(a.rows), (waves + 1) / 2 * 64, 0, s>>>(a);
+    else norm_long_kernel<T, OUT><<<grid_of(a.rows), kLongWaves * 64, 0, s>>>(a);
     return launched("norm_kernel");
 }
 
@@ -66,7 +66,7 @@ tcr_status backward(NormGrad a, hipStream_t s) {
     else if (items == 1) norm_grad_kernel<T, 0, 1><<<grid, block, 0, s>>>(a);
     else if (waves <= 2 * kMostWaves) norm_grad_kernel<T, 0, 2><<<grid, block, 0, s>>>(a);
     else {
-        if (a.rows != 0) norm_grad_long_kernel<T><<<dim3((unsigned)a.rows), kLongWaves * 64, 0, s>>>(a);
+        if (a.rows != 0) norm_grad_long_kernel<T><<<grid_of(a.rows), kLongWaves * 64, 0, s>>>(a);
         norm_weight_kernel<T><<<dim3((unsigned)(parts * div_up(a.cols, 64 * kVec))), 64, 0, s>>>(a);
     }
     if (launched("norm_grad_kernel") != TCR_OK) return TCR_ERR_HIP;

@@ -187,8 +187,8 @@ __global__ __launch_bounds__(LANES == 0 ? kMostWaves * 64 : kNormThreads) void n
     __shared__ float sums[kMostWaves];
     __shared__ uint32_t most[kMostWaves];
     const uint32_t lanes = LANES == 0 ? blockDim.x : LANES, lane = LANES == 0 ? threadIdx.x : threadIdx.x % LANES;
-    const uint64_t row = LANES == 0 ? blockIdx.x : (uint64_t)blockIdx.x * (kNormThreads / (LANES == 0 ? 1 : LANES)) + threadIdx.x / (LANES == 0 ? 1 : LANES);
-    if (row >= a.rows) return;                            // (whole groups of lanes, in kernels without barriers)
+    const uint64_t row = LANES == 0 ? workgroup() : (uint64_t)workgroup() * (kNormThreads / (LANES == 0 ? 1 : LANES)) + threadIdx.x / (LANES == 0 ? 1 : LANES);
+    if (row >= a.rows) return;                            // (whole groups of lanes, in kernels without barriers, or whole workgroups)
     const uint64_t cols = a.cols;
     const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
     const T* r = a.residual != nullptr ? static_cast<const T*>(a.residual) + (int64_t)row * a.r_stride : nullptr;
@@ -258,7 +258,8 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a
     constexpr uint64_t kStep = kLongWaves * 64 * kVec;
     __shared__ float sums[kLongWaves];
     __shared__ uint32_t most[kLongWaves];
-    const uint64_t row = blockIdx.x, cols = a.cols;
+    const uint64_t row = workgroup(), cols = a.cols;
+    if (row >= a.rows) return;                            // (whole workgroups)
     const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
     const T* r = a.residual != nullptr ? static_cast<const T*>(a.residual) + (int64_t)row * a.r_stride : nullptr;
     auto sum_at = [&](uint64_t col, float(&s)[kVec]) {
@@ -403,7 +404,8 @@ template <typename T>
 __global__ __launch_bounds__(kLongWaves * 64) void norm_grad_long_kernel(const NormGrad a) {
     constexpr uint64_t kStep = kLongWaves * 64 * kVec;
     __shared__ float sums[kLongWaves];
-    const uint64_t row = blockIdx.x, cols = a.cols;
+    const uint64_t row = workgroup(), cols = a.cols;
+    if (row >= a.rows) return;                            // (whole workgroups)
     const T* dy = static_cast<const T*>(a.dout) + (int64_t)row * a.dout_stride;
     const T* total = static_cast<const T*>(a.total) + (int64_t)row * a.total_stride;
     const T* more = a.dtotal != nullptr ? static_cast<const T*>(a.dtotal) + (int64_t)row * a.dtotal_stride : nullptr;

@@ -31,6 +31,12 @@ typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 inline bool on_boundary(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline uint64_t div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
+// A grid has fewer than 2^32 threads in each of its dimensions; of more, HIP starts what is left of the number modulo 2^32 and reports no error.  Workgroups that need more stand
+// in rows of kGridRow; those of the last row that nothing is left for end at once.
+constexpr uint32_t kGridRow = (1u << 22) - 1;    // (of up to 1024 threads each)
+inline dim3 grid_of(uint64_t blocks) { return blocks <= kGridRow ? dim3((unsigned)blocks) : dim3(kGridRow, (unsigned)div_up(blocks, kGridRow)); }
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridRow + blockIdx.x; }
+
 template <typename T> struct Bits;
 template <> struct Bits<_Float16> { typedef half8v v8; };
 template <> struct Bits<__bf16> { typedef bf8v v8; };
