@@ -258,7 +258,7 @@ tcr_status tcr_linear_attention_step(const tcr_attention *shape, const void *q, 
  * dfinal: the gradient of its final_state (NULL: none); dstate: the gradient of `state` (NULL: not wanted), not dfinal's array.
  * The decays are constants of a model and have no gradient here.  Where heads share keys and values the call needs tokens in all *
  * heads * max(dk, dv) floats of workspace, rounded up to a multiple of 64, in front of the states'.  Of a caller's buffer that is the second half of what follows its first
- * 256 bytes: a buffer of 256 + 8 bytes for each of these floats (and up to 128 MiB for the states) is enough; with less the call returns TCR_ERR_WORKSPACE, and
+ * 256 bytes: a buffer of 256 + 8 bytes for each of these floats (and up to 128 MiB for the states) is enough; with less of the former the call returns TCR_ERR_WORKSPACE, and
  * TCR_ERR_UNSUPPORTED where the stream is being recorded and its workspace is too small yet, and has done nothing.
  */
 tcr_status tcr_linear_attention_backward(const tcr_attention *shape, const void *dout, const void *q, const void *k, const void *v, void *dq, void *dk,

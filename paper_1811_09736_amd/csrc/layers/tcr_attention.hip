@@ -65,6 +65,9 @@ constexpr uint32_t kDirectBlocks = 8;
 // Wavefronts that a launch is cut for: two on each SIMD, or four where blocks stay long, for whose states' bytes more of them make up.  16 heads of 128 x 128,
 // two / four: 4 x 2048 tokens, gradients, blocks of 512 / 256 tokens 172 / 186 us; 32768 tokens, blocks of 2048 / 1024 tokens 244 / 230 us.
 constexpr uint64_t kFillWaves = 2048, kLongChunks = 16;
+// Floats of states between blocks that a call asks for at most.  Blocks are cut for the workgroups that fill the chip, each sequence into as many, so sequences and heads that
+// come close to that number by themselves would get twice of it: batches of 256 x 256 states 128 MiB.
+constexpr uint64_t kMostStates = (64ull << 20) / 4;
 
 // Workgroups for a kernel whose workgroups take the place of others behind the last.
 unsigned at_most(uint64_t blocks) { return (unsigned)(blocks < kGridRow ? blocks : kGridRow); }
@@ -101,9 +104,10 @@ struct Room {
     uint64_t count = 0;
 };
 
-// How a scan is cut: as many blocks as fill the chip, or as there are chunks or pairs of them; fewer where `most` floats do not hold their states.
+// How a scan is cut: as many blocks as fill the chip, or as there are chunks or pairs of them; fewer where `most` floats, or kMostStates, do not hold their states.
 // *need: the floats that these blocks want.
 Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need) {
+    if (most > kMostStates) most = kMostStates;
     const uint64_t slabs = div_up(a.dv, shape.cols), units = a.heads * slabs;
     const uint64_t spans = a.offsets != nullptr ? 1 : a.sequences;
     // (per block and unit a state, per block and head what is kept, two floats)

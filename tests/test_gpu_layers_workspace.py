@@ -1,5 +1,5 @@
-"""The workspace of linear attention's and the norm's gradients: refusals come before any work, and a recorded call that lacks room records
-nothing."""
+"""The workspace of linear attention's and the norm's gradients: refusals come before any work, a recorded call that lacks room records nothing, and states between
+blocks take no more than the header says."""
 import ctypes
 
 import pytest
@@ -102,3 +102,22 @@ def test_recording_norm_gradients_without_room(tcr):
     graph.replay()
     torch.cuda.synchronize()
     assert (dx == 7).all() and (dw == 7).all() and marker.item() == 1
+
+
+@pytest.mark.parametrize("batch,tokens,heads,dk,dv", [(15, 1024, 16, 256, 256), (9, 1024, 16, 256, 256), (3, 4096, 20, 200, 256), (1, 32768, 4, 256, 256),
+                                                      (7, 4096, 33, 128, 128), (31, 1024, 8, 128, 128), (5, 3000, 24, 128, 64), (1, 60000, 3, 64, 64)])
+def test_states_between_blocks_stay_within_64_mib(tcr, batch, tokens, heads, dk, dv):
+    q = torch.zeros(batch, tokens, heads, dk, device="cuda", dtype=torch.bfloat16)
+    v = torch.zeros(batch, tokens, heads, dv, device="cuda", dtype=torch.bfloat16)
+    decay, out, stream = torch.full((heads,), -0.01, device="cuda"), torch.empty_like(v), torch.cuda.Stream()
+    # (the stream's queue and the kernels are there before anything is measured, the workspace is not)
+    tcr.linear_attention(q[:1, :200], q[:1, :200], v[:1, :200], decay, out=out[:1, :200], stream=stream)
+    torch.cuda.synchronize()
+    tcr.release_stream(stream)
+    before = torch.cuda.mem_get_info()[0]
+    tcr.linear_attention(q, q, v, decay, out=out, stream=stream)
+    torch.cuda.synchronize()
+    taken = before - torch.cuda.mem_get_info()[0]
+    tcr.release_stream(stream)
+    # (memory is handed out in pieces of 2 MiB)
+    assert taken <= (64 << 20) + (2 << 20), taken / 2 ** 20
