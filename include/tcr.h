@@ -220,7 +220,7 @@ tcr_status tcr_scan(const void *in, float *out, uint64_t n, void *stream);
  *   (stride[0] is not used); offsets is a DEVICE pointer to sequences + 1 non-decreasing token indices as in the irregular calls
  *   above, not validated either.  Rows of out whose token lies in no sequence are set to 0.
  * log_decay: DEVICE pointer to `heads` floats, the natural logarithm of what is kept of S from one token to the next (0: all
- * of it, minus infinity: nothing).
+ * of it, minus infinity: nothing; NaN: the head's results are NaN).
  * state, final_state: DEVICE pointers, 16-byte aligned, sequences x heads x dk x dv floats each, contiguous; the state in front
  * of the first token and behind the last (of an empty sequence: the same).  NULL: zeros, and not wanted.  They must be different arrays.
  * dk and dv: multiples of 8 from 8 to 256; fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED otherwise).  The magnitude of

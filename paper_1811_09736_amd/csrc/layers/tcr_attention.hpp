@@ -38,8 +38,11 @@ struct Scan {
     uint32_t reverse, late;
 };
 
-// The natural logarithm of a head's decay; minus infinity (nothing is kept) as a number whose product with 0 is 0.
-__device__ __forceinline__ float decay_of(const Scan& a, uint32_t h) { return fmaxf(a.log_decay[h], -1e30f); }
+// The natural logarithm of a head's decay; minus infinity (nothing is kept) as a number whose product with 0 is 0.  (NaN stays, and with it all that the head decays.)
+__device__ __forceinline__ float decay_of(const Scan& a, uint32_t h) {
+    const float d = a.log_decay[h];
+    return d < -1e30f ? -1e30f : d;
+}
 // decay^steps
 __device__ __forceinline__ float decayed(float log_decay, float steps) { return expf(log_decay * steps); }
 // A state is multiplied by the same decay^steps chunk after chunk (token after token, block after block).  Near 1 the rounding of that one number, 2^-25, would add up over all
