@@ -31,7 +31,10 @@ class _LinearAttention(torch.autograd.Function):
 
 
 def linear_attention(q, k, v, log_decay, scale=None, offsets=None, state=None):
-    """binding.linear_attention with gradients for q, k, v and state: (out, the states behind the last tokens)."""
+    """binding.linear_attention with gradients for q, k, v and state: (out, the states behind the last tokens).  log_decay is a constant: one that
+    requires a gradient, and would never get it, is refused."""
+    if log_decay.requires_grad and torch.is_grad_enabled():
+        raise ValueError("log_decay must not require a gradient: the decays are constants of the model here (pass log_decay.detach())")
     return _LinearAttention.apply(q, k, v, log_decay, scale, offsets, state)
 
 
