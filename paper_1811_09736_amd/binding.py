@@ -481,6 +481,13 @@ def _ptr(x: Optional[torch.Tensor]):
     return None if x is None else x.data_ptr()
 
 
+def _written(*given: Optional[torch.Tensor]) -> None:
+    """Tensors of the caller's that a call has written through their pointers: autograd is to notice where it has kept them."""
+    for x in given:
+        if x is not None:
+            torch.autograd.graph.increment_version(x)
+
+
 def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, scale: Optional[float] = None,
                      offsets: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None, final_state: bool = False,
                      out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
@@ -493,6 +500,7 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
         got = _native.linear_attention(q, k, v, log_decay, scale, offsets, state, final_state, out)
         if got is not None:
             return got
+    given = out
     if out is None:
         out = torch.empty(*q.shape[:-1], v.shape[-1], dtype=q.dtype, device=q.device)
     shape = _attention(q, k, v, out, log_decay, scale, offsets)
@@ -502,6 +510,7 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     last = torch.empty(states, dtype=torch.float32, device=q.device) if final_state else None
     _run(_lib.tcr_linear_attention, "tcr_linear_attention", q, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
          _ptr(state), _ptr(last))
+    _written(given)
     return (out, last) if final_state else out
 
 
@@ -514,6 +523,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         got = _native.linear_attention_step(q, k, v, log_decay, scale, None, state, new_state, out)
         if got is not None:
             return got
+    given = out
     if out is None:
         out = torch.empty(*q.shape[:-1], v.shape[-1], dtype=q.dtype, device=q.device)
     shape = _attention(q, k, v, out, log_decay, scale, None, step=True)
@@ -525,6 +535,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         _states_of(new_state, "new_state", states, q)
     _run(_lib.tcr_linear_attention_step, "tcr_linear_attention_step", q, stream, shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
          state.data_ptr(), new_state.data_ptr())
+    _written(new_state, given)
     return out
 
 

@@ -46,6 +46,10 @@ uint32_t type_of(at::ScalarType t) { return t == at::kHalf ? TCR_F16 : t == at::
 PyObject* wrapped(const at::Tensor& t) { return THPVariable_Wrap(t); }
 c10::TensorOptions options_of(const at::Tensor& x, at::ScalarType t) { return x.options().dtype(t).requires_grad(false); }
 void* data_of(const at::Tensor* t) { return t != nullptr ? t->data_ptr() : nullptr; }
+// A tensor of the caller's that a call has written through its pointer: autograd is to notice where it has kept it.
+void written(const at::Tensor* t) {
+    if (t != nullptr && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 
 // ------------------------------------------------------------------------------------------------ attention
 struct Attention {
@@ -143,6 +147,7 @@ PyObject* linear_attention(PyObject*, PyObject* const* args, Py_ssize_t count) {
              g_linear_attention(&a.shape, a.q->data_ptr(), a.k->data_ptr(), a.v->data_ptr(), out.data_ptr(), static_cast<const float*>(data_of(state)),
                                 last.defined() ? static_cast<float*>(last.data_ptr()) : nullptr, stream))
     if (st != TCR_OK) return failed(st, "tcr_linear_attention");
+    written(given);
     return last.defined() ? Py_BuildValue("NN", wrapped(out), wrapped(last)) : wrapped(out);
     END_HANDLE_TH_ERRORS
 }
@@ -161,7 +166,10 @@ PyObject* linear_attention_step(PyObject*, PyObject* const* args, Py_ssize_t cou
     TCR_CALL((out = given != nullptr ? *given : a.make_output(true)),
              g_linear_attention_step(&a.shape, a.q->data_ptr(), a.k->data_ptr(), a.v->data_ptr(), out.data_ptr(),
                                      static_cast<const float*>(state->data_ptr()), to, stream))
-    return st == TCR_OK ? wrapped(out) : failed(st, "tcr_linear_attention_step");
+    if (st != TCR_OK) return failed(st, "tcr_linear_attention_step");
+    written(next != nullptr ? next : state);
+    written(given);
+    return wrapped(out);
     END_HANDLE_TH_ERRORS
 }
 
