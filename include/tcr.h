@@ -223,6 +223,8 @@ tcr_status tcr_scan(const void *in, float *out, uint64_t n, void *stream);
  * of it, minus infinity: nothing; NaN: the head's results are NaN).
  * state, final_state: DEVICE pointers, 16-byte aligned, sequences x heads x dk x dv floats each, contiguous; the state in front
  * of the first token and behind the last (of an empty sequence: the same).  NULL: zeros, and not wanted.  They must be different arrays.
+ * out may stand among the rows of q, k and v (parts of one buffer's rows), never in their place: other workgroups read them while it is written.
+ * Overlaps are refused (TCR_ERR_INVALID_ARG) where rows without gaps show them, or equal first rows.
  * dk and dv: multiples of 8 from 8 to 256; fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED otherwise).  The magnitude of
  * scale lies between 1e-18 and 1e18.  As everywhere, inputs are finite: an infinity or NaN poisons its own sequence, also up to
  * 63 tokens in front of it.

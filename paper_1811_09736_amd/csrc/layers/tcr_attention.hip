@@ -187,14 +187,50 @@ tcr_status run(const Scan& a, uint32_t dtype, bool wide, hipStream_t stream, con
 
 tcr_status check_states(const void* a, const void* b) { return on_boundary(a, 16) && on_boundary(b, 16) ? TCR_OK : TCR_ERR_INVALID_ARG; }
 
+// The memory of an array of rows: its bytes, where the rows fill them without gaps.
+struct Extent {
+    uintptr_t from, to;
+    bool whole;
+};
+Extent extent(const tcr_attention& a, const void* p, const int64_t stride[3], uint64_t heads, uint64_t d) {
+    const uint64_t counts[3] = {a.offsets != nullptr ? 1 : a.sequences, a.tokens, heads};
+    __int128 reach = d, all = d;                   // (strides may be anything)
+    bool whole = true;
+    for (int i = 0; i < 3; ++i) {
+        if (counts[i] > 1 && stride[i] < 0) whole = false;
+        reach += (__int128)(counts[i] - 1) * stride[i];
+        all *= counts[i];
+    }
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+    whole = whole && reach == all;
+    return {from, whole ? from + (uintptr_t)(2 * all) : from + 2 * d, whole};
+}
+// Whether two of them share memory for certain.  (Rows with gaps may stand in each other's; they are only looked at where they start.)
+bool share(const Extent& a, const Extent& b) { return a.whole && b.whole ? a.from < b.to && b.from < a.to : a.from == b.from; }
+// The same of two arrays of states.
+bool states_share(const tcr_attention& a, const float* x, const float* y) {
+    if (x == nullptr || y == nullptr) return false;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y), bytes = 4 * a.sequences * a.heads * a.dk * a.dv;
+    return x == y || (p < q + bytes && q < p + bytes);
+}
+
 bool odd(const void* p) { return p == nullptr || !on_boundary(p, 2); }
 
-tcr_status forward(const tcr_attention* shape, const void* q, const void* k, const void* v, void* out, const float* state, float* final_state,
+// step: final_state may be `state`
+tcr_status forward(const tcr_attention* shape, const void* q, const void* k, const void* v, void* out, const float* state, float* final_state, bool step,
                    hipStream_t stream) {
     tcr_status st = check(shape);
     if (st != TCR_OK) return st;
     const bool any = shape->tokens != 0 && (shape->sequences != 0 || shape->offsets != nullptr);
     if ((any && (odd(q) || odd(k) || odd(v) || odd(out))) || check_states(state, final_state) != TCR_OK) return TCR_ERR_INVALID_ARG;
+    // (other workgroups read the rows of q, k and v that one has written out for: those of other columns, of heads that share them, of blocks behind)
+    if (any) {
+        const Extent written = extent(*shape, out, shape->o_stride, shape->heads, shape->dv);
+        if (share(written, extent(*shape, q, shape->q_stride, shape->heads, shape->dk)) || share(written, extent(*shape, k, shape->k_stride, shape->kv_heads, shape->dk)) ||
+            share(written, extent(*shape, v, shape->v_stride, shape->kv_heads, shape->dv)))
+            return TCR_ERR_INVALID_ARG;
+    }
+    if ((state != final_state || !step) && states_share(*shape, state, final_state)) return TCR_ERR_INVALID_ARG;
     const uint32_t group = shape->heads / shape->kv_heads;
     const bool packed = shape->offsets != nullptr;
     Scan s = scan_of(*shape, view(q, shape->q_stride, 1, packed), view(k, shape->k_stride, group, packed), view(v, shape->v_stride, group, packed), out,
@@ -210,7 +246,7 @@ tcr_status backward(const tcr_attention* shape, const void* dout, const void* q,
     if (st != TCR_OK) return st;
     const bool any = shape->tokens != 0 && (shape->sequences != 0 || shape->offsets != nullptr);
     if (any && (odd(dout) || odd(q) || odd(k) || odd(v) || odd(dq) || odd(dk) || odd(dv))) return TCR_ERR_INVALID_ARG;
-    if (check_states(state, dfinal) != TCR_OK || check_states(dstate, nullptr) != TCR_OK) return TCR_ERR_INVALID_ARG;
+    if (check_states(state, dfinal) != TCR_OK || check_states(dstate, nullptr) != TCR_OK || states_share(*shape, dstate, dfinal)) return TCR_ERR_INVALID_ARG;
     const tcr_attention& a = *shape;
     const uint32_t group = a.heads / a.kv_heads;
     const bool packed = a.offsets != nullptr;
@@ -301,8 +337,7 @@ tcr_status guarded(F f) {
 extern "C" tcr_status tcr_linear_attention(const tcr_attention* shape, const void* q, const void* k, const void* v, void* out, const float* state,
                                            float* final_state, void* stream) {
     return guarded([&] {
-        if (shape != nullptr && state != nullptr && state == final_state) return TCR_ERR_INVALID_ARG;
-        return forward(shape, q, k, v, out, state, final_state, static_cast<hipStream_t>(stream));
+        return forward(shape, q, k, v, out, state, final_state, false, static_cast<hipStream_t>(stream));
     });
 }
 
@@ -310,14 +345,13 @@ extern "C" tcr_status tcr_linear_attention_step(const tcr_attention* shape, cons
                                                 float* new_state, void* stream) {
     return guarded([&] {
         if (shape != nullptr && (shape->tokens != 1 || shape->offsets != nullptr || state == nullptr || new_state == nullptr)) return TCR_ERR_INVALID_ARG;
-        return forward(shape, q, k, v, out, state, new_state, static_cast<hipStream_t>(stream));
+        return forward(shape, q, k, v, out, state, new_state, true, static_cast<hipStream_t>(stream));
     });
 }
 
 extern "C" tcr_status tcr_linear_attention_backward(const tcr_attention* shape, const void* dout, const void* q, const void* k, const void* v, void* dq,
                                                     void* dk, void* dv, const float* state, const float* dfinal, float* dstate, void* stream) {
     return guarded([&] {
-        if (dstate != nullptr && dstate == dfinal) return TCR_ERR_INVALID_ARG;
         return backward(shape, dout, q, k, v, dq, dk, dv, state, dfinal, dstate, static_cast<hipStream_t>(stream));
     });
 }
