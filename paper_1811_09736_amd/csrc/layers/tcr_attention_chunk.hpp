@@ -590,9 +590,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
         // ---- the state behind the chunk
         float factor_c = 1.0f;
         if constexpr (kHalf) {
-            largest_c = wave_largest(largest_c);
-            // (values that two parts hold to 22 bits as they are stay as they are)
-            if (!(largest_c >= 0.125f && largest_c < 32768.0f)) factor_c = near_top(largest_c);
+            // (also where the largest is at home in binary16: two parts hold 21 bits of what lies within 2^18 of the top, and of smaller values none that lie below 2^-25)
+            factor_c = near_top(wave_largest(largest_c));
         }
         // (what the chunk adds is summed apart and comes to S at once: one rounding of its size a chunk, and not one for each product.  The decay is rounded so
         // that it makes up for what the roundings of the ones before it have left out: its own is the same in every chunk)
@@ -635,7 +634,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
             if (W == 8) read_rows(0);
             f4v add[kBatch][NT];
             // (negated twice: an instruction with a negated operand keeps S in its place, without one the sum goes to the place of `add` and 32 registers do not fit)
-            const float minus = settled(-decay * factor_c);
+            const float minus = settled(-decay), back = reciprocal_power(factor_c);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 const int ks = i % KS, m0 = i / KS * kBatch;
@@ -654,14 +653,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) S[m0 + m][nt][r] = fmaf(-S[m0 + m][nt][r], minus, add[m][nt][r]);
-            }
-            if (kHalf && factor_c != 1.0f) {
-                const float f = reciprocal_power(factor_c);
-#pragma unroll
-                for (int mt = 0; mt < KT; ++mt)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) S[mt][nt] *= f;
+                            for (int r = 0; r < 4; ++r) S[m0 + m][nt][r] = fmaf(-S[m0 + m][nt][r], minus, kHalf ? add[m][nt][r] * back : add[m][nt][r]);
             }
         }
         if (!STATES && now.last && a.fin != nullptr) {
