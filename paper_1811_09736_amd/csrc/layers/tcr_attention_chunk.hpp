@@ -323,14 +323,14 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
         for (uint32_t m = blocks.direct ? in_front : block - 1; m < block; ++m) {
             const Kept keep = m == in_front || !blocks.direct ? Kept{0.0f, 0.0f} : blocks.keep[(uint64_t)h * (blocks.count - 1) + m];
             const float* const from = blocks.states + ((int64_t)h * head_states + m) * kStateSize;
-            if (nothing(keep)) clear();                             // (NaN ends with its sequence)
+            f4v x[KT][NT];
 #pragma unroll
             for (int mt = 0; mt < KT; ++mt)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    f4v x = {0, 0, 0, 0};
+                    x[mt][nt] = f4v{0, 0, 0, 0};
                     if (!blocks.turned) {
-                        x = *reinterpret_cast<const f4v*>(from + (int64_t)slab * (blocks.count - 1) * kStateSize + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
+                        x[mt][nt] = *reinterpret_cast<const f4v*>(from + (int64_t)slab * (blocks.count - 1) * kStateSize + ((w * KT + mt) * NT + nt) * 256 + lane * 4);
                     } else {
                         // (row k, column v of this S is row v, column k there)
                         const uint32_t v = slab * kSlab + (w * NT + nt) * 16 + n;
@@ -339,12 +339,18 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
                             const uint32_t k = mt * 16 + 4 * g + r;
                             const float* there = from + (int64_t)(k / kSlab) * (blocks.count - 1) * kStateSize +
                                                  ((k % kSlab / (16 * NT) * KT + v / 16) * NT + k / 16 % NT) * 256 + (v % 16 / 4 * 16 + k % 16) * 4 + v % 4;
-                            if (k < a.dk) x[r] = *there;
+                            if (k < a.dk) x[mt][nt][r] = *there;
                         }
                     }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = kept_plus(keep, S[mt][nt][r], x[r]);
                 }
+            loads_first();                                          // (the state does not wait for what is kept of the ones in front)
+            if (nothing(keep)) clear();                             // (NaN ends with its sequence)
+#pragma unroll
+            for (int mt = 0; mt < KT; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[mt][nt][r] = kept_plus(keep, S[mt][nt][r], x[mt][nt][r]);
         }
     }
 
@@ -537,6 +543,12 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
 #pragma unroll
                     for (int r = 0; r < 8; ++r) largest_c = fmaxf(largest_c, fabsf((float)cols[ks][nt][r]));
             }
+        float factor_c = 1.0f;
+        if constexpr (kHalf) {
+            // (here, and not where it is used: a factor is the same for a wavefront, the largest value of each lane would take up a vector register meanwhile.  Also where
+            // the largest is at home in binary16: two parts hold 21 bits of what lies within 2^18 of the top, and of smaller values none that lie below 2^-25)
+            factor_c = uniform(near_top(wave_largest(largest_c)));
+        }
         if constexpr (!STATES) {
             constexpr bool kNextToo = W != 8;                                      // (as registers allow)
             v8 scores[2][CT];                                                      // one part of 32 columns, and the next on its way
@@ -588,11 +600,6 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
         }
 
         // ---- the state behind the chunk
-        float factor_c = 1.0f;
-        if constexpr (kHalf) {
-            // (also where the largest is at home in binary16: two parts hold 21 bits of what lies within 2^18 of the top, and of smaller values none that lie below 2^-25)
-            factor_c = near_top(wave_largest(largest_c));
-        }
         // (what the chunk adds is summed apart and comes to S at once: one rounding of its size a chunk, and not one for each product.  The decay is rounded so
         // that it makes up for what the roundings of the ones before it have left out: its own is the same in every chunk)
         if (STATES || (now.last ? a.fin != nullptr : more)) {                      // (a state that nothing follows is not worked out)
