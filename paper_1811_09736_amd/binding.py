@@ -495,7 +495,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
 
     q [B, T, H, dk], k [B, T, G, dk], v [B, T, G, dv], H a multiple of G; or packed sequences [N, H, dk] ... with `offsets`
     ([sequences + 1], int64).  log_decay [H], float32.  scale: dk ** -0.5 if not given.  state [sequences, H, dk, dv], float32: the
-    states to go on from.  Returns out [B, T, H, dv] ([N, H, dv]), with final_state also the states behind the last tokens."""
+    states to go on from.  Returns out [B, T, H, dv] ([N, H, dv]; a given one not in the place of q, k or v), with final_state also the
+    states behind the last tokens."""
     if stream is None:
         got = _native.linear_attention(q, k, v, log_decay, scale, offsets, state, final_state, out)
         if got is not None:

@@ -55,15 +55,15 @@ Scan scan_of(const tcr_attention& a, const View& va, const View& vb, const View&
 }
 
 // Tokens of a sequence up to which its states go from token to token in registers, each token a pass over them, and not through a chunk's products, which take
-// the same for 1 and for 32 tokens.  16 heads of 128 x 128, steps / chunk: 1 sequence, 4 tokens 6.7 / 9.0 us, 8 tokens 10.0 / 9.0;
-// 256 sequences, 2 tokens 130 / 132, 4 tokens 177 / 134.
+// the same for 1 and for 32 tokens.  16 heads of 128 x 128, steps / chunk: 1 sequence, 4 tokens 6.9 / 9.1 us, 8 tokens 10.3 / 9.1;
+// 256 sequences, 2 tokens 129 / 127, 4 tokens 177 / 129.
 constexpr uint64_t kStepTokens = 2, kFewStepTokens = 4, kFewPairs = 32;
 constexpr uint64_t kWholeChunks = 2;
 // Blocks of a sequence up to which each adds up the states in front of it by itself, without a kernel for the carries.  16 heads of 128 x 128: 4 x 2048 tokens in
-// 8 blocks each 60 us, with that kernel 72; 16 blocks 32.9 and 33.0.  States that are read transposed are read in pieces of 16 bytes: once, not for each block.
+// 8 blocks each 62 us, with that kernel 70; 2048 tokens in 16 blocks 33.2 and 32.3.  States that are read transposed are read in pieces of 16 bytes: once, not for each block.
 constexpr uint32_t kDirectBlocks = 8;
 // Wavefronts that a launch is cut for: two on each SIMD, or four where blocks stay long, for whose states' bytes more of them make up.  16 heads of 128 x 128,
-// two / four: 4 x 2048 tokens, gradients, blocks of 512 / 256 tokens 172 / 186 us; 32768 tokens, blocks of 2048 / 1024 tokens 244 / 230 us.
+// two / four: 2 x 4096 tokens, blocks of 512 / 256 tokens 65 / 75 us; 8 x 2048 tokens, 1024 / 512 tokens 115 / 104; 32768 tokens, 2048 / 1024 tokens 235 / 225.
 constexpr uint64_t kFillWaves = 2048, kLongChunks = 16;
 // Floats of states between blocks that a call asks for at most.  Blocks are cut for the workgroups that fill the chip, each sequence into as many, so sequences and heads that
 // come close to that number by themselves would get twice of it: batches of 256 x 256 states 128 MiB.
@@ -118,7 +118,7 @@ Blocks cut(const Scan& a, const ChunkShape& shape, uint64_t most, uint64_t* need
     uint64_t per_span = div_up(2 * kFillWaves / shape.waves, units * spans);
     if (chunks < per_span * kLongChunks) per_span = div_up(kFillWaves / shape.waves, units * spans);
     // (the kernel for the states takes as long as a chunk or two: sequences of so many stay whole.  Of one chunk where each block adds up the others' states,
-    // of two where that would be too many: 1024 tokens in 8 blocks of two chunks 23 us, in 16 of one 31.)
+    // of two where that would be too many: 1024 tokens in 8 blocks of two chunks 24 us, in 16 of one 31.)
     const uint64_t most_blocks = chunks <= kWholeChunks ? 1 : chunks <= kDirectBlocks ? chunks : pairs;
     if (per_span > most_blocks) per_span = most_blocks;
     if (per_span > 1 && per_span * spans > most / each + 1) {
@@ -161,7 +161,8 @@ tcr_status run_chunks(const Scan& a, const Room& given, hipStream_t stream) {
     return launched("attention_chunk_kernel");
 }
 
-// Whether chunks take a scan, or it goes token by token.  (Packed sequences: by their mean.)
+// Whether chunks take a scan, or it goes token by token.  (Packed sequences: by their mean, as only the device knows more of their lengths.  A long one among many of one token
+// goes the way of the others: 1000 tokens behind 1000 single ones, 16 heads of 128 x 128, take 2.7 ms token by token, 1.1 ms by chunks; 256 single tokens 0.11 and 0.53 ms.)
 bool by_chunks(const Scan& a) {
     const uint64_t steps = a.sequences * a.heads <= kFewPairs ? kFewStepTokens : kStepTokens;
     if (a.sequences == 0 || a.total <= steps * a.sequences) return false;

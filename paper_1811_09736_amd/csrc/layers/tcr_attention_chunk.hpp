@@ -10,9 +10,9 @@
 // several blocks: a first kernel (STATES) leaves the state that each block alone arrives at, a second adds up what
 // reaches each block from the ones in front, and this one starts from there.
 //
-// MI355X, 32768 tokens, 16 heads of 128 x 128, bfloat16: states 65 us, carries 15, this 144, for 965 MB in all.  A workgroup alone takes 10 000 cycles for a chunk, two
-// on a compute unit 13 700 for a chunk each: rows into LDS 1 000, asking for the next ones 300 to 1 000, scores 2 000, products with the state 1 200, with
-// the scores 1 000, stores 500, the state 2 000, the rest at barriers; vector ALUs are busy for 37 %, LDS for 30 %, matrix cores for 25 % of the time.
+// MI355X, 32768 tokens, 16 heads of 128 x 128, bfloat16, 227 us: states 68, carries 16, this 143, 929 MB and 155 GFLOP (all parts) in all, which a copy and a large product would take
+// 175 and 118 us for.  Two workgroups on a compute unit take 10 200 cycles for a chunk each: vector ALUs are busy for 46 %, LDS for 43 % (12 % in bank conflicts, see ChunkLds),
+// matrix cores for 30 % of the time, in turn between barriers.
 // Eight wavefronts of 16 columns on 128 registers beat four of 32 columns on 256 by 5 to 8 % although each of them reads all of a and b from LDS.
 //
 // Layouts.  v_mfma_f32_16x16x32: lane l = n + 16 g gives A[n][8g .. 8g+7] and B[8g .. 8g+7][n] and receives D[4g .. 4g+3][n].
@@ -25,8 +25,8 @@
 //
 // Rounding.  The matrix cores take 16-bit operands.  a, b and c are theirs exactly; the derived ones would cost the results half of
 // their precision if they were rounded: scores and S as a factor are given as two parts (high + low, 2 products, off by 2^-17 of themselves in bfloat16 and
-// 2^-20 in binary16, for outputs that are rounded by 2^-9 and 2^-12), decayed c, whose sums are the binary32 states, as three bfloat16 or two binary16 parts (2^-21 at most).
-// The gradients' states too, so that a gradient is the same whether the states' own is asked for or not (two bfloat16 parts for them: gradients of 4 x 2048 tokens, 16 heads of 128 x 128, 170 us instead of 181).
+// 2^-20 in binary16 at most, for outputs that are rounded by up to 2^-8 and 2^-11), decayed c, whose sums are the binary32 states, as three bfloat16 or two binary16 parts (2^-21 at most).
+// The gradients' states too, so that a gradient is the same whether the states' own is asked for or not (two bfloat16 parts for them: gradients of 4 x 2048 tokens, 16 heads of 128 x 128, 170 us instead of 181, 192 on another machine).
 // binary16 holds neither large nor small values, so scores, S and c are brought near 2^14 by powers of two there.
 #pragma once
 #include "tcr_attention.hpp"
@@ -190,7 +190,8 @@ __device__ __forceinline__ float reciprocal_power(float f) { return __builtin_bi
 
 template <typename T, int DK, int COLS, int C>
 struct ChunkLds {
-    // (rows 16 bytes beyond a multiple of 128: reads of 8 or 16 bytes from 16 rows meet no bank twice; 32 bytes: reads of columns)
+    // (rows 16 bytes beyond a multiple of 128: reads of 8 or 16 bytes from 16 rows meet no bank twice; 32 bytes: reads of columns do not, those of rows meet the banks of rows n
+    // and n + 8 twice -- of b and of the scores, a quarter of all LDS cycles)
     static constexpr int kStrideA = DK + 8, kStrideB = DK + 16, kStrideC = COLS + 16, kStrideP = C + 16;
     alignas(16) T b[C * kStrideB];
     alignas(16) T c[C * kStrideC];
@@ -586,8 +587,9 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint32_t v = (w * NT + nt) * 16 + 4 * g;
-                    // (the tile's offset is added here and not given as the store's scalar one: 16-byte stores of that form lost their first
-                    // elements to the instructions behind them in a few lanes)
+                    // (the tile's offset is added here and not given as the store's scalar one: 16-byte stores of that form, binary32 outputs, lost their first
+                    // elements in a few lanes: the registers of a store of more than 8 bytes must not be written right behind it, and the compiler keeps that
+                    // distance for the form without a scalar offset only)
                     const uint32_t behind = (reverse ? CT - 1 - it : it) * pitch;
                     const uint32_t at = it * 16 + n < now.len && v < left ? (at_row + v) * (uint32_t)sizeof(OUT) + behind : kOutside;
                     typedef OUT o4 __attribute__((ext_vector_type(4)));
@@ -606,6 +608,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 2, W
             const int steps = now.len - late;
             const float power = lds.powers[steps], owed = lds.missed[steps] + missed, decay = power + owed;
             missed = uniform(owed - (decay - power));
+            // (a chunk of up to 32 tokens takes the second half's rows of zeros along, 0.5 us: a branch around them sends 12 registers and more to memory)
             constexpr int kBatch = W == 8 ? 2 : 4;                                 // (as registers allow)
             constexpr int kSteps = KT / kBatch * KS;
             v8 rows[2][kBatch];                                                    // of these 32 tokens and kBatch * 16 rows of S, and the next on their way

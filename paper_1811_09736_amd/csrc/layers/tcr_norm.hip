@@ -13,7 +13,7 @@ namespace {
 constexpr uint64_t kMostRows = 1ull << 31, kMostCols = 1ull << 24;
 
 // Lanes of 8 columns for a row of up to 512, several rows a workgroup; then a workgroup of as many wavefronts as hold the row, up to 8 of them with 8 columns
-// a lane, then with 16.  (5120 columns: 5 wavefronts of 16 a lane 56.6 us for 8191 rows in 8 bits, 10 of 8 a lane 68; 4096: 4 of 16 96.5 us for 16384 rows, 8 of 8 93.9.)
+// a lane, then with 16.  (5120 columns: 5 wavefronts of 16 a lane 57.0 us for 8191 rows in 8 bits, 10 of 8 a lane 68; 4096: 4 of 16 96.5 us for 16384 rows, 8 of 8 93.9.)
 template <typename T, int OUT>
 tcr_status run(const Norm& a, hipStream_t s) {
     const unsigned waves = (unsigned)div_up(a.cols, 64 * kVec);

@@ -180,7 +180,7 @@ __device__ __forceinline__ void store_codes(uint8_t* row, uint64_t col, uint64_t
 }
 
 // ITEMS vectors per lane; LANES lanes per row and 256 / LANES rows per workgroup, or (0) a row per workgroup, of as many wavefronts as hold it.
-// MI355X: 16384 x 4096 bfloat16 with the residual, 537 MB, in 90 us, 6.0 TB/s: what a copy reaches.
+// MI355X: 16384 x 4096 bfloat16 with the residual, 537 MB, in 93.5 us, 5.7 TB/s, where a copy reaches 5.2 to 5.5.
 constexpr int kNormThreads = 256, kMostWaves = 16;
 template <typename T, int OUT, int LANES, int ITEMS>
 __global__ __launch_bounds__(LANES == 0 ? kMostWaves * 64 : kNormThreads) void norm_kernel(const Norm a) {
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kLongWaves * 64) void norm_long_kernel(const Norm a
 }
 
 // Gradients: a row per wavefront and four per workgroup (LANES == 64), or a row per workgroup (0); each takes every parts-th of them, the next
-// row's loads on their way meanwhile, and keeps its sums of dweight in registers.  MI355X: 16384 x 4096 bfloat16, 537 MB, in 99 us and 5 for the parts, 5.1 TB/s
+// row's loads on their way meanwhile, and keeps its sums of dweight in registers.  MI355X: 16384 x 4096 bfloat16, 537 MB, in 98 us and 5 for the parts, 5.2 TB/s
 // (166 without the loads ahead, with four wavefronts of 16 columns a lane).
 template <typename T, int LANES, int ITEMS>
 __global__ __launch_bounds__(LANES == 0 ? kMostWaves * 64 : kNormThreads) void norm_grad_kernel(const NormGrad a) {
