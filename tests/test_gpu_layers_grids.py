@@ -10,8 +10,13 @@ def tcr():
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     from paper_1811_09736_amd import binding
-    yield binding
-    torch.cuda.empty_cache()                 # (tens of GiB that later tests in this process may want to see free)
+    return binding
+
+
+@pytest.fixture(autouse=True)
+def free_afterwards():
+    yield
+    torch.cuda.empty_cache()                 # (tens of GiB that the next test may want to see free)
 
 
 def parts(n):
