@@ -297,6 +297,39 @@ tcr_status tcr_rms_norm_backward(const void *dout, const void *total, const void
                                  uint32_t dtype, uint32_t weight_dtype, void *stream);
 
 /*
+ * Selective state space scan: `states` running values for every channel, restarted for every sequence, whose factors depend on the data.
+ *   d_t = softplus(dt_t + dt_bias)  (softplus == 0: dt_t + dt_bias),
+ *   h_t[n] = exp(d_t a[n]) h_{t-1}[n] + d_t x_t b_t[n]        (binary32; h before the first token is `state`, or 0)
+ *   y_t = sum_n c_t[n] h_t[n] + skip x_t,   out_t = y_t, or y_t gate_t / (1 + exp(-gate_t)).
+ * tcr_selective says what the arrays hold.  x, dt, gate and out hold one row of `channels` consecutive elements for every token, of the type
+ * `dtype` (TCR_F16, TCR_BF16, TCR_F32); row (sequence b, token t) starts b * stride[0] + t * stride[1] ELEMENTS behind the pointer.  b and c hold
+ * one row of `states` elements for every token and group, group g stride[2] elements behind group 0; channel i goes with group i / (channels / groups).
+ * gate == NULL: none.  a: channels x states floats, contiguous; skip, dt_bias: `channels` floats each, or NULL (zeros).  DEVICE pointers.
+ *   offsets == NULL: `sequences` sequences of `tokens` tokens each; otherwise packed ones, as in tcr_linear_attention.  Rows of out whose token lies in
+ *   no sequence are set to 0.
+ * state, final_state: DEVICE pointers, sequences x channels x states floats each, contiguous; the states in front of the first token and behind the last
+ * (of an empty sequence: the same).  NULL: zeros, and not wanted.  They must be different arrays, and out none of the inputs (TCR_ERR_INVALID_ARG where rows
+ * without gaps show it, or equal first rows).
+ * 1 <= states <= 64, channels <= 2^20, a multiple of groups; fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED beyond).  An infinity or NaN of a token stays in its
+ * sequence, from that token on, and in its channel (of b and c: its group).
+ * Results are the same from run to run.  Workspace: where sequences and channels are too few to fill the chip, tokens are cut into chunks whose states pass through it,
+ * 64 chunks of a sequence at most; with less of it, or none, the call takes fewer chunks and longer, and its sums other roundings.
+ */
+typedef struct {
+    uint32_t dtype, channels, states, groups, softplus;
+    uint64_t sequences, tokens;
+    const uint64_t *offsets;
+    const float *a, *skip, *dt_bias;
+    int64_t x_stride[2], dt_stride[2], gate_stride[2], o_stride[2], b_stride[3], c_stride[3];
+} tcr_selective;
+
+tcr_status tcr_selective_scan(const tcr_selective *shape, const void *x, const void *dt, const void *b, const void *c, const void *gate, void *out,
+                              const float *state, float *final_state, void *stream);
+/* One token for every sequence (tokens == 1, offsets == NULL): out and the states behind it.  new_state may be `state`. */
+tcr_status tcr_selective_scan_step(const tcr_selective *shape, const void *x, const void *dt, const void *b, const void *c, const void *gate, void *out,
+                                   const float *state, float *new_state, void *stream);
+
+/*
  * Bench / test hook: choose among measured alternatives.  Keys and values:
  *   "formulation"  "mfma" (default: matrix-core products) | "dpp" (cross-lane wavefront primitives)
  *   "scan_carry"   "lookback" (default: single pass, decoupled look-back) | "reduce_then_scan" |

@@ -32,6 +32,7 @@ EXPORTS = (
     "tcr_set_variant", "tcr_segmented_scan_noalloc",
     "tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward",
     "tcr_rms_norm", "tcr_rms_norm_quantized", "tcr_rms_norm_backward",
+    "tcr_selective_scan", "tcr_selective_scan_step",
     "tcr_kernel_name", "tcr_check_device_flags", "tcr_release", "tcr_release_stream", "tcr_status_string", "tcr_last_hip_error",
 )
 
@@ -45,6 +46,13 @@ class AttentionShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_uint32) for n in ("dtype", "heads", "kv_heads", "dk", "dv")] + [
         ("sequences", ctypes.c_uint64), ("tokens", ctypes.c_uint64), ("offsets", ctypes.c_void_p), ("log_decay", ctypes.c_void_p),
         ("scale", ctypes.c_float)] + [(n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride", "o_stride")]
+
+
+class SelectiveShape(ctypes.Structure):
+    """tcr_selective."""
+    _fields_ = [(n, ctypes.c_uint32) for n in ("dtype", "channels", "states", "groups", "softplus")] + [
+        ("sequences", ctypes.c_uint64), ("tokens", ctypes.c_uint64)] + [(n, ctypes.c_void_p) for n in ("offsets", "a", "skip", "dt_bias")] + [
+        (n, ctypes.c_int64 * 2) for n in ("x_stride", "dt_stride", "gate_stride", "o_stride")] + [(n, ctypes.c_int64 * 3) for n in ("b_stride", "c_stride")]
 
 
 class TcrError(RuntimeError):
@@ -104,6 +112,11 @@ def _load() -> ctypes.CDLL:
     lib.tcr_rms_norm_backward.argtypes = [vp] * 7 + [u64, u64, i64, i64, i64, u32, u32, vp]
     for name in ("tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward", "tcr_rms_norm", "tcr_rms_norm_quantized",
                  "tcr_rms_norm_backward"):
+        getattr(lib, name).restype = ctypes.c_int
+    scan = ctypes.POINTER(SelectiveShape)
+    lib.tcr_selective_scan.argtypes = [scan] + [vp] * 9
+    lib.tcr_selective_scan_step.argtypes = [scan] + [vp] * 9
+    for name in ("tcr_selective_scan", "tcr_selective_scan_step"):
         getattr(lib, name).restype = ctypes.c_int
     lib.tcr_workspace_bytes.argtypes = [ctypes.c_int, u64, u64]
     lib.tcr_workspace_bytes.restype = u64
@@ -644,6 +657,102 @@ def rms_norm_backward(dout: torch.Tensor, total: torch.Tensor, weight: torch.Ten
     _run(_lib.tcr_rms_norm_backward, "tcr_rms_norm_backward", total, stream, dout.data_ptr(), total.data_ptr(), weight.data_ptr(), rstd.data_ptr(),
          _ptr(dtotal), dx.data_ptr(), dweight.data_ptr(), rows, cols, ds, ts, ms, _DTYPES[total.dtype], _DTYPES[weight.dtype])
     return dx, dweight
+
+
+# ------------------------------------------------------------------------------ selective state space scan
+def _tokens_of(x, name: str, shape, dtype, like):
+    """Strides of the leading dimensions of [sequence, token, ...], packed or for one token [token or sequence, ...]."""
+    if not (x.is_cuda and x.dtype == dtype and x.device == like.device and tuple(x.shape) == tuple(shape) and (x.stride(-1) == 1 or x.shape[-1] == 1)):
+        raise TypeError(f"{name} must be a {dtype} CUDA tensor of shape {tuple(shape)} on x's device whose last dimension is contiguous")
+    return x.stride()
+
+
+def _constants_of(x, name: str, shape, like) -> None:
+    if x is not None and not (x.is_cuda and x.dtype == torch.float32 and x.is_contiguous() and x.device == like.device and tuple(x.shape) == tuple(shape)):
+        raise TypeError(f"{name} must be a contiguous float32 CUDA tensor of shape {tuple(shape)} on x's device")
+
+
+def _two(stride, packed: bool, step: bool, dims: int):
+    """(sequence, token) strides, with a third for the groups where there are any (dims == 2)."""
+    lead = stride[:len(stride) - 1]
+    rest = lead[-1:] if dims == 2 else ()
+    if step:
+        return (ctypes.c_int64 * (1 + dims))(lead[0], 0, *rest)
+    return (ctypes.c_int64 * (1 + dims))(*((0, lead[0]) if packed else lead[:2]), *rest)
+
+
+def _token_input(x, offsets, step: bool):
+    """(sequences, tokens) of x: [sequence, token, channel], packed [token, channel], for one token [sequence, channel]."""
+    if not (x.is_cuda and x.dtype in (torch.float16, torch.bfloat16, torch.float32)):
+        raise TypeError("x must be a float16, bfloat16 or float32 CUDA tensor")
+    if x.dim() != (3 if offsets is None and not step else 2) or x.shape[-1] < 1:
+        raise ValueError(f"x has the shape {tuple(x.shape)}; expected [sequences, tokens, channels], packed [tokens, channels] with offsets, "
+                         "for one token [sequences, channels]")
+    if offsets is not None:
+        return _check_offsets(x, offsets), x.shape[0]
+    return (x.shape[0], 1) if step else x.shape[:2]
+
+
+def _selective(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, out, step=False):
+    """The checked tcr_selective of a call."""
+    sequences, tokens = _token_input(x, offsets, step)
+    channels = x.shape[-1]
+    packed = offsets is not None
+    if a.dim() != 2 or b.dim() != x.dim() + 1 or b.shape[-2] < 1 or channels % b.shape[-2] != 0:
+        raise ValueError(f"shapes do not fit: x {tuple(x.shape)}, a {tuple(a.shape)}, b {tuple(b.shape)}")
+    states, groups = a.shape[-1], b.shape[-2]
+    _constants_of(a, "a", (channels, states), x)
+    _constants_of(skip, "skip", (channels,), x)
+    _constants_of(dt_bias, "dt_bias", (channels,), x)
+    rows = [_two(_tokens_of(t, name, x.shape, x.dtype, x), packed, step, 1) if t is not None else (ctypes.c_int64 * 2)()
+            for t, name in ((x, "x"), (dt, "dt"), (gate, "gate"), (out, "out"))]
+    groups_of = [_two(_tokens_of(t, name, (*x.shape[:-1], groups, states), x.dtype, x), packed, step, 2) for t, name in ((b, "b"), (c, "c"))]
+    return SelectiveShape(_DTYPES[x.dtype], channels, states, groups, 1 if softplus else 0, sequences, tokens, _ptr(offsets), a.data_ptr(), _ptr(skip),
+                          _ptr(dt_bias), *rows, *groups_of)
+
+
+def selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, skip: Optional[torch.Tensor] = None,
+                   gate: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None, softplus: bool = True,
+                   offsets: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None, final_state: bool = False,
+                   out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """tcr_selective_scan: h_t = exp(d_t a) h_{t-1} + d_t x_t b_t with d_t = softplus(dt_t + dt_bias); y_t = sum of c_t h_t over the states +
+    skip x_t; out_t = y_t, with a gate y_t gate_t sigmoid(gate_t).
+
+    x, dt, gate [B, T, D], b, c [B, T, G, N], D a multiple of G; or packed sequences [M, D], [M, G, N] with `offsets` ([sequences + 1], int64).  a [D, N],
+    skip, dt_bias [D], float32.  softplus=False: d_t = dt_t + dt_bias.  state [sequences, D, N], float32: the states to go on from.
+    Returns out [B, T, D] ([M, D]; a given one none of the inputs), with final_state also the states behind the last tokens."""
+    given = out
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    shape = _selective(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, out)
+    states = (shape.sequences, shape.channels, shape.states)
+    _constants_of(state, "state", states, x)
+    last = torch.empty(states, dtype=torch.float32, device=x.device) if final_state else None
+    _run(_lib.tcr_selective_scan, "tcr_selective_scan", x, stream, shape, x.data_ptr(), dt.data_ptr(), b.data_ptr(), c.data_ptr(), _ptr(gate),
+         out.data_ptr(), _ptr(state), _ptr(last))
+    _written(given)
+    return (out, last) if final_state else out
+
+
+def selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, state: torch.Tensor,
+                        skip: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None,
+                        softplus: bool = True, new_state: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """tcr_selective_scan_step: one token for every sequence.  x, dt, gate [B, D], b, c [B, G, N], state [B, D, N].  The new states go to new_state,
+    without it to `state` itself.  Returns out [B, D]."""
+    given = out
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    shape = _selective(x, dt, a, b, c, skip, gate, dt_bias, softplus, None, out, step=True)
+    states = (shape.sequences, shape.channels, shape.states)
+    if new_state is None:
+        new_state = state
+    for t, name in ((state, "state"), (new_state, "new_state")):
+        _constants_of(t, name, states, x)
+    _run(_lib.tcr_selective_scan_step, "tcr_selective_scan_step", x, stream, shape, x.data_ptr(), dt.data_ptr(), b.data_ptr(), c.data_ptr(), _ptr(gate),
+         out.data_ptr(), state.data_ptr(), new_state.data_ptr())
+    _written(new_state, given)
+    return out
 
 
 def workspace_bytes(op: int, n: int, seg_len: int) -> int:

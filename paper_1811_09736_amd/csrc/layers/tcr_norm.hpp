@@ -13,7 +13,6 @@
 namespace tcr {
 namespace layers {
 
-constexpr int kVec = 8;                        // elements a lane loads at once: 16 bytes of 16-bit types
 constexpr float kSmallestScale = 1.17549435e-38f;
 
 enum NormOut { kNormSame = 0, kNormE4M3 = 1, kNormI8 = 2 };
@@ -39,46 +38,6 @@ struct NormGrad {
     uint32_t weight_wide, parts;
 };
 
-// Vectors of kVec elements that need no more alignment than an element.
-template <typename T> struct Vec;
-template <> struct Vec<_Float16> { typedef _Float16 v __attribute__((ext_vector_type(8), aligned(2))); };
-template <> struct Vec<__bf16> { typedef __bf16 v __attribute__((ext_vector_type(8), aligned(2))); };
-template <> struct Vec<float> { typedef float v __attribute__((ext_vector_type(8), aligned(4))); };
-
-// The same as they are in memory.
-template <typename T>
-__device__ __forceinline__ typename Vec<T>::v load_raw(const T* row, uint64_t col, uint64_t cols) {
-    if (col + kVec <= cols) return *reinterpret_cast<const typename Vec<T>::v*>(row + col);
-    typename Vec<T>::v x;
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) x[i] = col + i < cols ? row[col + i] : (T)0.0f;
-    return x;
-}
-// Columns col .. col + 7 of a row, 0 beyond its end.
-template <typename T>
-__device__ __forceinline__ void load_vec(const T* row, uint64_t col, uint64_t cols, float (&v)[kVec]) {
-    if (col + kVec <= cols) {
-        const typename Vec<T>::v x = *reinterpret_cast<const typename Vec<T>::v*>(row + col);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = (float)x[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = col + i < cols ? (float)row[col + i] : 0.0f;
-    }
-}
-template <typename T>
-__device__ __forceinline__ void store_vec(T* row, uint64_t col, uint64_t cols, const float (&v)[kVec]) {
-    if (col + kVec <= cols) {
-        typename Vec<T>::v x;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = (T)v[i];
-        *reinterpret_cast<typename Vec<T>::v*>(row + col) = x;
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (col + i < cols) row[col + i] = (T)v[i];
-    }
-}
 template <typename T>
 __device__ __forceinline__ void load_weight(const void* w, uint32_t wide, uint64_t col, uint64_t cols, float (&v)[kVec]) {
     if (wide) load_vec(static_cast<const float*>(w), col, cols, v);

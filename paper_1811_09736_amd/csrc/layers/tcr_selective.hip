@@ -1,0 +1,152 @@
+// Host side of the selective scan: checks, how it is cut, which kernels run.
+#include "tcr_selective.hpp"
+#include "tcr_operands.hpp"
+
+using namespace tcr;
+using namespace tcr::layers;
+using tcr::host::launched;
+using tcr::host::partials_for;
+
+namespace {
+
+constexpr uint64_t kMostTokens = 1ull << 31;       // in all; keeps every token index in range
+constexpr uint32_t kMostStates = 64, kMostChannels = 1u << 20;
+
+// Wavefronts that a scan is cut for, and chunks of a sequence at most: each looks through the ones in front of it.
+constexpr uint64_t kFillWaves = 2048, kMostChunks = 64;
+
+template <typename T, int K, int P>
+tcr_status run(Selective s, hipStream_t stream) {
+    constexpr uint32_t kTile = 8 * P, kStates = K * P, kChannels = Slab<P>::kChannels;
+    const uint64_t spans = s.offsets != nullptr ? 1 : s.sequences;
+    if (spans == 0) return TCR_OK;
+    s.slabs = (uint32_t)div_up(s.channels / s.groups, kChannels);
+    const uint64_t slabs = (uint64_t)s.slabs * s.groups, all = slabs * kChannels, each = spans * all * (kStates + 1);
+    uint64_t chunks = div_up(kFillWaves / 4, spans * slabs);
+    if (chunks > kMostChunks) chunks = kMostChunks;
+    auto cut = [&] {
+        s.length = (uint32_t)(div_up(div_up(s.span, chunks), kTile) * kTile);
+        if (s.length == 0) s.length = kTile;
+        s.per_span = (uint32_t)div_up(s.span, s.length);
+        if (s.per_span == 0) s.per_span = 1;
+    };
+    cut();
+    if (s.per_span > 1) {
+        uint64_t got = 0;
+        const tcr_status st = partials_for(stream, (s.per_span - 1) * each, 0, &s.ends, &got);
+        if (st != TCR_OK) return st;
+        if (got < (s.per_span - 1) * each) {
+            chunks = got / each + 1;
+            cut();
+        }
+        s.sums = s.ends + (s.per_span - 1) * spans * all * kStates;
+    }
+    if (s.per_span > 1) {
+        const uint64_t blocks = slabs * spans * (s.per_span - 1);
+        selective_kernel<T, K, P, false><<<grid_of(blocks), kScanThreads, 0, stream>>>(s, (uint32_t)blocks);
+        if (launched("selective_kernel<states>") != TCR_OK) return TCR_ERR_HIP;
+    }
+    const uint64_t blocks = slabs * spans * s.per_span;
+    selective_kernel<T, K, P, true><<<grid_of(blocks), kScanThreads, 0, stream>>>(s, (uint32_t)blocks);
+    return launched("selective_kernel");
+}
+
+template <typename T>
+tcr_status run(const Selective& s, hipStream_t stream) {
+    if (s.states <= 4) return run<T, 4, 1>(s, stream);
+    if (s.states <= 8) return run<T, 4, 2>(s, stream);
+    if (s.states <= 16) return run<T, 4, 4>(s, stream);
+    if (s.states <= 32) return run<T, 4, 8>(s, stream);
+    return run<T, 4, 16>(s, stream);
+}
+
+template <typename T, int P>
+tcr_status step(const Selective& s, hipStream_t stream) {
+    const uint32_t whole = s.states == 4 * P && on_boundary(s.state, 16) && on_boundary(s.fin, 16) && on_boundary(s.a, 16);
+    const uint64_t blocks = s.sequences * div_up(s.channels, kScanThreads / P);
+    if (blocks == 0) return TCR_OK;
+    selective_step_kernel<T, P><<<grid_of(blocks), kScanThreads, 0, stream>>>(s, whole);
+    return launched("selective_step_kernel");
+}
+template <typename T>
+tcr_status step(const Selective& s, hipStream_t stream) {
+    if (s.states <= 4) return step<T, 1>(s, stream);
+    if (s.states <= 8) return step<T, 2>(s, stream);
+    if (s.states <= 16) return step<T, 4>(s, stream);
+    if (s.states <= 32) return step<T, 8>(s, stream);
+    return step<T, 16>(s, stream);
+}
+
+tcr_status check(const tcr_selective* a) {
+    if (a == nullptr || a->dtype > TCR_F32 || a->channels == 0 || a->states == 0 || a->groups == 0 || a->channels % a->groups != 0 || a->softplus > 1)
+        return TCR_ERR_INVALID_ARG;
+    if (a->a == nullptr || !on_boundary(a->a, 4) || !on_boundary(a->skip, 4) || !on_boundary(a->dt_bias, 4) || !on_boundary(a->offsets, 8)) return TCR_ERR_INVALID_ARG;
+    if (a->states > kMostStates || a->channels > kMostChannels || a->sequences >= kMostTokens || total_tokens(*a) >= kMostTokens) return TCR_ERR_UNSUPPORTED;
+    return TCR_OK;
+}
+
+Operand operand(const void* p, const int64_t* stride, bool packed, int64_t group = 0) { return {p, packed ? 0 : stride[0], stride[1], group}; }
+
+Selective arguments(const tcr_selective& a, const void* x, const void* dt, const void* b, const void* c, const void* gate) {
+    const bool packed = a.offsets != nullptr;
+    Selective s = {};
+    s.x = operand(x, a.x_stride, packed);
+    s.dt = operand(dt, a.dt_stride, packed);
+    s.gate = operand(gate, a.gate_stride, packed);
+    s.b = operand(b, a.b_stride, packed, a.b_stride[2]);
+    s.c = operand(c, a.c_stride, packed, a.c_stride[2]);
+    s.out_seq = packed ? 0 : a.o_stride[0];
+    s.out_tok = a.o_stride[1];
+    s.a = a.a;
+    s.skip = a.skip;
+    s.bias = a.dt_bias;
+    s.offsets = a.offsets;
+    s.sequences = a.sequences;
+    s.span = (uint32_t)a.tokens;
+    s.channels = a.channels;
+    s.states = a.states;
+    s.groups = a.groups;
+    s.softplus = a.softplus;
+    return s;
+}
+
+tcr_status forward(const tcr_selective* shape, const void* x, const void* dt, const void* b, const void* c, const void* gate, void* out, const float* state,
+                   float* last, bool one, hipStream_t stream) {
+    const tcr_status st = check(shape);
+    if (st != TCR_OK) return st;
+    const tcr_selective& a = *shape;
+    const uintptr_t size = a.dtype == TCR_F32 ? 4 : 2;
+    if (!on_boundary(state, 4) || !on_boundary(last, 4)) return TCR_ERR_INVALID_ARG;
+    if (total_tokens(a) != 0) {
+        if (missing(x, size) || missing(dt, size) || missing(b, size) || missing(c, size) || missing(out, size) || !on_boundary(gate, size)) return TCR_ERR_INVALID_ARG;
+        // (other workgroups read what one has written out for: b and c, and in the states' kernel all of them)
+        const Extent written = extent(a, out, a.o_stride, a.channels, size);
+        if (share(written, extent(a, x, a.x_stride, a.channels, size)) || share(written, extent(a, dt, a.dt_stride, a.channels, size)) ||
+            share(written, extent(a, b, a.b_stride, a.states, size, a.groups)) || share(written, extent(a, c, a.c_stride, a.states, size, a.groups)) ||
+            (gate != nullptr && share(written, extent(a, gate, a.gate_stride, a.channels, size))))
+            return TCR_ERR_INVALID_ARG;
+    }
+    const uint64_t bytes = 4 * a.sequences * (uint64_t)a.channels * a.states;
+    if ((state != last || !one) && arrays_share(state, bytes, last, bytes)) return TCR_ERR_INVALID_ARG;
+    Selective s = arguments(a, x, dt, b, c, gate);
+    s.out = out;
+    s.state = state;
+    s.fin = last;
+    if (one) return a.dtype == TCR_F16 ? step<_Float16>(s, stream) : a.dtype == TCR_BF16 ? step<__bf16>(s, stream) : step<float>(s, stream);
+    return a.dtype == TCR_F16 ? run<_Float16>(s, stream) : a.dtype == TCR_BF16 ? run<__bf16>(s, stream) : run<float>(s, stream);
+}
+
+}  // namespace
+
+extern "C" tcr_status tcr_selective_scan(const tcr_selective* shape, const void* x, const void* dt, const void* b, const void* c, const void* gate, void* out,
+                                         const float* state, float* final_state, void* stream) {
+    return guarded([&] { return forward(shape, x, dt, b, c, gate, out, state, final_state, false, static_cast<hipStream_t>(stream)); });
+}
+
+extern "C" tcr_status tcr_selective_scan_step(const tcr_selective* shape, const void* x, const void* dt, const void* b, const void* c, const void* gate, void* out,
+                                              const float* state, float* new_state, void* stream) {
+    return guarded([&] {
+        if (shape != nullptr && (shape->tokens != 1 || shape->offsets != nullptr || state == nullptr || new_state == nullptr)) return TCR_ERR_INVALID_ARG;
+        return forward(shape, x, dt, b, c, gate, out, state, new_state, true, static_cast<hipStream_t>(stream));
+    });
+}

@@ -1,0 +1,399 @@
+// Selective state space scan: a segmented scan whose factors depend on the data, `states` running values a channel.
+//
+//     d_t = softplus(dt_t + bias),   h_t[n] = exp(d_t a[n]) h_{t-1}[n] + d_t x_t b_t[n],   y_t = sum_n c_t[n] h_t[n] + skip x_t,
+//     out_t = y_t, or y_t gate_t sigmoid(gate_t).
+// a, skip, bias: by channel; b, c: by token, shared by the channels of a group.  Everything between loads and stores is binary32.
+//
+// A workgroup takes a slab of channels and a chunk of tokens, tile by tile.  P lanes hold a channel, each K of its states in registers for the
+// whole chunk; what a token needs of its channel (d and d x) and of its group (b, c) stands in LDS as binary32, made once by whole vectors.
+// What bounds it is the vector unit: an exponential (3.2 times a multiply-add), two multiplications and two multiply-adds for each state.
+#pragma once
+#include "tcr_shared.hpp"
+
+namespace tcr {
+namespace layers {
+
+constexpr int kScanThreads = 256;
+constexpr int kTokens = 4;                     // a turn of the inner loop
+
+struct Operand {                               // of the rows of a sequence's tokens; strides in elements
+    const void* p;
+    int64_t seq, tok, group;
+};
+
+struct Selective {
+    Operand x, dt, gate, b, c;                 // gate.p: NULL for none
+    void* out;
+    int64_t out_seq, out_tok;
+    const float *a, *skip, *bias, *state;      // skip, bias, state: NULL for none
+    float* fin;                                // the states behind the last tokens; NULL: not wanted
+    const uint64_t* offsets;
+    uint64_t sequences;
+    float *ends, *sums;                        // of every chunk: [chunk][padded channel][padded state] the state behind it from nothing, [chunk][padded channel] the sum of d
+    uint32_t span, length, per_span;           // tokens of a span (a sequence, or all packed ones), of a chunk; chunks of a span
+    uint32_t channels, states, groups, slabs;  // slabs of a group
+    uint32_t softplus;
+};
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// log(1 + e) for e in [0, 1] as 2 atanh(e / (2 + e)); the series ends at s^17, s <= 1/3: 2 s^19 / 19 < 2^-32 of it.  Two roundings more than
+// the sum's own, and none of it lost where e is small.
+__device__ __forceinline__ float log1p_unit(float e) {
+    const float r0 = __builtin_amdgcn_rcpf(2.0f + e);
+    const float s = e * __builtin_fmaf(__builtin_fmaf(-(2.0f + e), r0, 1.0f), r0, r0), q = s * s;
+    float v = 2.0f / 17.0f;
+    v = __builtin_fmaf(v, q, 2.0f / 15.0f);
+    v = __builtin_fmaf(v, q, 2.0f / 13.0f);
+    v = __builtin_fmaf(v, q, 2.0f / 11.0f);
+    v = __builtin_fmaf(v, q, 2.0f / 9.0f);
+    v = __builtin_fmaf(v, q, 2.0f / 7.0f);
+    v = __builtin_fmaf(v, q, 2.0f / 5.0f);
+    v = __builtin_fmaf(v, q, 2.0f / 3.0f);
+    return __builtin_fmaf(s * q, v, 2.0f * s);
+}
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float softplus_of(float x) { return (x > 0.0f ? x : 0.0f) + log1p_unit(exp_of(-__builtin_fabsf(x))); }
+// 1 / (1 + exp(-x)): from 0 at minus infinity to 1.
+__device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }
+
+// Where the sequences of a span begin and end.  bound(i) never leaves the span, whatever the offsets hold.
+struct Bounds {
+    const uint64_t* offsets;
+    uint32_t count, span;
+    __device__ __forceinline__ uint32_t at(uint32_t i) const {
+        const uint64_t o = offsets[i];
+        return o < span ? (uint32_t)o : span;
+    }
+    // How many of the count + 1 bounds are at most t.
+    __device__ __forceinline__ uint32_t upto(uint32_t t) const {
+        uint32_t low = 0, high = count + 1;
+        while (low < high) {
+            const uint32_t mid = low + (high - low) / 2;
+            if (at(mid) <= t) low = mid + 1;
+            else high = mid;
+        }
+        return low;
+    }
+};
+
+// The sequence that a token of a span stands in, and where the next bound is.
+struct Place {
+    uint32_t seq, next;                        // next: the first bound behind the token (none: ~0)
+    uint32_t start;
+    bool inside;
+    __device__ __forceinline__ void find(const Bounds& b, uint32_t span_index, uint32_t t) {
+        if (b.offsets == nullptr) {
+            seq = span_index, start = 0, next = b.span, inside = true;
+            return;
+        }
+        const uint32_t n = b.upto(t);
+        inside = n >= 1 && n <= b.count;
+        seq = n - 1;
+        start = inside ? b.at(seq) : 0;
+        next = n <= b.count ? b.at(n) : ~0u;
+    }
+    // Over the bound at t, and over empty sequences there.
+    __device__ __forceinline__ void pass(const Bounds& b, uint32_t t) {
+        do ++seq;
+        while (seq < b.count && b.at(seq + 1) <= t);
+        inside = seq < b.count;
+        start = t;
+        next = inside ? b.at(seq + 1) : ~0u;
+    }
+};
+
+// The states n0 .. n0 + K - 1 of a channel in an array [sequence][channel][state]; 0 where there is no array or no such state.
+template <int K>
+__device__ __forceinline__ void load_states(const float* states, uint64_t seq, const Selective& s, uint32_t ch, uint32_t n0, bool real, float (&h)[K]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) h[k] = states != nullptr && real && n0 + k < s.states ? states[(seq * s.channels + ch) * s.states + n0 + k] : 0.0f;
+}
+template <int K>
+__device__ __forceinline__ void store_states(float* states, uint64_t seq, const Selective& s, uint32_t ch, uint32_t n0, bool real, const float (&h)[K]) {
+    if (states == nullptr || !real) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (n0 + k < s.states) states[(seq * s.channels + ch) * s.states + n0 + k] = h[k];
+}
+
+// Sums of y[0 .. 3] over the P lanes of a channel (lane = part * (64 / P) + channel).  Lanes swap halves, so that each step has half as many values left:
+// lane part p ends with the sum of token sum_token<P>(p, i) in y[i], i < sum_count<P>.
+template <int P> constexpr int sum_count = P == 1 ? 4 : P == 2 ? 2 : 1;
+template <int P>
+__device__ __forceinline__ int sum_token(int lane, int i) {
+    if (P == 1) return i;
+    if (P == 2) return (lane >> 5) + 2 * i;
+    return (lane >> 5) + 2 * ((lane >> 4) & 1);
+}
+__device__ __forceinline__ float swap_add32(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+    const uint32_t low = r[0], high = r[1];                // (a bit_cast of r[1] itself reads r[0])
+    return __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
+}
+__device__ __forceinline__ float swap_add16(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+    const uint32_t low = r[0], high = r[1];                // (a bit_cast of r[1] itself reads r[0])
+    return __builtin_bit_cast(float, low) + __builtin_bit_cast(float, high);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_of(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false));
+}
+constexpr int kRor4 = 0x124, kRor8 = 0x128;
+template <int P>
+__device__ __forceinline__ void sum_parts(float (&y)[kTokens]) {
+    if (P == 1) return;
+    y[0] = swap_add32(y[0], y[1]);
+    y[1] = swap_add32(y[2], y[3]);
+    if (P == 2) return;
+    y[0] = swap_add16(y[0], y[1]);
+    if (P >= 8) y[0] += dpp_of<kRor8>(y[0]);
+    if (P >= 16) y[0] += dpp_of<kRor4>(y[0]);
+}
+// The same of one value: every lane has the sum.
+template <int P>
+__device__ __forceinline__ float sum_one(float y) {
+#pragma unroll
+    for (int m = 32; m >= 64 / P; m >>= 1) y += __shfl_xor(y, m);
+    return y;
+}
+
+// How a workgroup stands in the grid: slab of channels fastest, so that neighbours read neighbouring columns of the same tokens.
+template <int P>
+struct Slab {
+    static constexpr int kWide = 64 / P, kChannels = 4 * kWide;
+    uint32_t chunk, span, group, first, end, padded;       // first, end: channels; padded: the slab's place among padded channels
+    __device__ __forceinline__ Slab(const Selective& s, uint32_t chunks) {
+        const uint32_t all = s.slabs * s.groups, each = s.channels / s.groups, block = workgroup();
+        const uint32_t slab = block % all, rest = block / all;
+        chunk = rest % chunks;
+        span = rest / chunks;
+        group = slab / s.slabs;
+        first = group * each + (slab % s.slabs) * kChannels;
+        end = (group + 1) * each;
+        padded = slab * kChannels;
+    }
+};
+
+// OUT: outputs and last states; otherwise a chunk's state from nothing and its sum of d, for the chunks behind it.
+template <typename T, int K, int P, bool OUT>
+__global__ __launch_bounds__(kScanThreads) void selective_kernel(Selective s, uint32_t blocks) {
+    constexpr int kWide = 64 / P, kChannels = 4 * kWide, kTile = 8 * P, kStates = K * P, kRow = kChannels / kVec;
+    constexpr int kShared = kTile * kStates / kScanThreads > 0 ? kTile * kStates / kScanThreads : 1;
+    static_assert(kTile * kRow == kScanThreads, "one vector of a tile for each thread");
+    __shared__ float du[kTile][kChannels][2];              // d, d x; then y in the place of d
+    __shared__ float bs[kTile][kStates], cs[OUT ? kTile : 1][kStates];
+    if (workgroup() >= blocks) return;
+    const Slab<P> slab(s, OUT ? s.per_span : s.per_span - 1);
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wide = (tid >> 6) * kWide + lane % kWide, n0 = lane / kWide * K;
+    const uint32_t ch = slab.first + wide;
+    const bool real = ch < slab.end;
+    const uint64_t spans = s.offsets != nullptr ? 1 : s.sequences, all = (uint64_t)s.slabs * s.groups * kChannels;
+    const uint32_t t0 = slab.chunk * s.length, t1 = s.span - t0 < s.length ? s.span : t0 + s.length;
+    const Bounds bounds = {s.offsets, (uint32_t)s.sequences, s.span};
+    Place at;
+    at.find(bounds, slab.span, t0);
+
+    float rate[K], h[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) rate[k] = real && n0 + k < s.states ? s.a[(uint64_t)ch * s.states + n0 + k] * kLog2e : 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) h[k] = 0.0f;
+    if (at.inside && at.start == t0) load_states(s.state, at.seq, s, ch, n0, real, h);
+    else if (OUT && at.inside) {
+        // the state that the chunks in front leave, back to the one in which the sequence begins
+        uint32_t i = at.start / s.length;
+        const uint64_t one = spans * all;
+        const uint64_t place = slab.span * all + slab.padded + wide;
+        auto end_of = [&](uint32_t c, int k) { return s.ends[(c * one + place) * kStates + n0 + k]; };
+#pragma unroll
+        for (int k = 0; k < K; ++k) h[k] = end_of(i, k);
+        for (++i; i < slab.chunk; ++i) {
+            const float sum = s.sums[i * one + place];
+#pragma unroll
+            for (int k = 0; k < K; ++k) h[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(sum * rate[k]), h[k], end_of(i, k));
+        }
+    }
+
+    // what this thread puts into LDS: eight channels of one of a tile's tokens, and some of b and c
+    const uint32_t my_token = tid / kRow, my_wide = tid % kRow * kVec, my_first = slab.first + my_wide;
+    const uint32_t my_end = slab.end;
+    const T* const x_row = static_cast<const T*>(s.x.p) + slab.span * s.x.seq;
+    const T* const dt_row = static_cast<const T*>(s.dt.p) + slab.span * s.dt.seq;
+    const T* const gate_row = static_cast<const T*>(s.gate.p) + slab.span * s.gate.seq;
+    const T* const b_row = static_cast<const T*>(s.b.p) + slab.span * s.b.seq + slab.group * s.b.group;
+    const T* const c_row = static_cast<const T*>(s.c.p) + slab.span * s.c.seq + slab.group * s.c.group;
+    T* const out_row = static_cast<T*>(s.out) + slab.span * s.out_seq;
+    const bool gated = OUT && s.gate.p != nullptr;
+    float bias[kVec], skip[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        bias[i] = s.bias != nullptr && my_first + i < my_end ? s.bias[my_first + i] : 0.0f;
+        skip[i] = OUT && s.skip != nullptr && my_first + i < my_end ? s.skip[my_first + i] : 0.0f;
+    }
+    const uint32_t begin = s.offsets != nullptr ? bounds.at(0) : 0, finish = s.offsets != nullptr ? bounds.at(bounds.count) : s.span;
+
+    typedef typename Vec<T>::v vec;
+    vec x_next = {}, dt_next = {}, gate_next = {};
+    T b_next[kShared] = {}, c_next[kShared] = {};
+    auto fetch = [&](uint32_t tile) {
+        const uint32_t t = tile + my_token;
+        const bool there = t < t1 && my_first < my_end;
+        x_next = there ? load_raw(x_row + t * s.x.tok, my_first, my_end) : vec{};
+        dt_next = there ? load_raw(dt_row + t * s.dt.tok, my_first, my_end) : vec{};
+        if (gated) gate_next = there ? load_raw(gate_row + t * s.gate.tok, my_first, my_end) : vec{};
+#pragma unroll
+        for (int i = 0; i < kShared; ++i) {
+            const uint32_t e = tid + i * kScanThreads, bt = tile + e / kStates, n = e % kStates;
+            const bool any = e < kTile * kStates && bt < t1 && n < s.states;
+            b_next[i] = any ? b_row[bt * s.b.tok + n] : (T)0.0f;
+            if (OUT) c_next[i] = any ? c_row[bt * s.c.tok + n] : (T)0.0f;
+        }
+    };
+    float sum = 0.0f;
+    if (t0 < t1) fetch(t0);
+    for (uint32_t tile = t0; tile < t1; tile += kTile) {
+        const vec x_now = x_next, gate_now = gate_next;
+        const bool there = tile + my_token < t1;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float raw = (float)dt_next[i] + bias[i], d = s.softplus ? softplus_of(raw) : raw;
+            // (behind the chunk: the states stay)
+            du[my_token][my_wide + i][0] = there ? d : 0.0f;
+            du[my_token][my_wide + i][1] = there ? d * (float)x_now[i] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kShared; ++i) {
+            const uint32_t e = tid + i * kScanThreads;
+            if (e >= kTile * kStates) break;
+            bs[e / kStates][e % kStates] = (float)b_next[i];
+            if (OUT) cs[e / kStates][e % kStates] = (float)c_next[i];
+        }
+        __syncthreads();
+        if (tile + kTile < t1) fetch(tile + kTile);
+
+        auto token = [&](uint32_t j) {
+            const float d = du[j][wide][0], u = du[j][wide][1];
+            float y = 0.0f;
+            if (!OUT) sum += d;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                h[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * rate[k]), h[k], u * bs[j][n0 + k]);
+                if (OUT) y = __builtin_fmaf(cs[j][n0 + k], h[k], y);
+            }
+            return y;
+        };
+        const uint32_t here = t1 - tile < kTile ? t1 - tile : kTile;
+        for (uint32_t j = 0; j < here; j += kTokens) {
+            const uint32_t t = tile + j;
+            if (at.next >= t + kTokens || at.next >= t1) {
+                float y[kTokens];
+#pragma unroll
+                for (int i = 0; i < kTokens; ++i) y[i] = token(j + i);
+                if (OUT) {
+                    sum_parts<P>(y);
+#pragma unroll
+                    for (int i = 0; i < sum_count<P>; ++i) du[j + sum_token<P>(lane, i)][wide][0] = y[i];
+                }
+                continue;
+            }
+            for (uint32_t i = 0; i < kTokens && t + i < t1; ++i) {
+                if (at.next == t + i) {
+                    if (OUT && at.inside) store_states(s.fin, at.seq, s, ch, n0, real, h);
+                    at.pass(bounds, t + i);
+                    if (at.inside) load_states(s.state, at.seq, s, ch, n0, real, h);
+                }
+                const float y = sum_one<P>(token(j + i));
+                if (OUT && lane < kWide) du[j + i][wide][0] = y;
+            }
+        }
+        __syncthreads();
+        if (OUT && there && my_first < my_end) {
+            const uint32_t t = tile + my_token;
+            float v[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                v[i] = __builtin_fmaf(skip[i], (float)x_now[i], du[my_token][my_wide + i][0]);
+                if (gated) {
+                    const float z = (float)gate_now[i];
+                    v[i] *= z * sigmoid_of(z);
+                }
+                if (t < begin || t >= finish) v[i] = 0.0f;
+            }
+            store_vec(out_row + t * s.out_tok, my_first, my_end, v);
+        }
+    }
+    if constexpr (OUT) {
+        if (at.inside && at.next == t1) store_states(s.fin, at.seq, s, ch, n0, real, h);
+        if (s.offsets != nullptr && s.fin != nullptr)
+            for (uint32_t e = slab.chunk; e < bounds.count; e += s.per_span)
+                if (bounds.at(e + 1) <= bounds.at(e)) {
+                    load_states(s.state, e, s, ch, n0, real, h);
+                    store_states(s.fin, e, s, ch, n0, real, h);
+                }
+    } else {
+        const uint64_t place = (slab.chunk * spans + slab.span) * all + slab.padded + wide;
+#pragma unroll
+        for (int k = 0; k < K; ++k) s.ends[place * kStates + n0 + k] = h[k];
+        if (lane < kWide) s.sums[place] = sum;
+    }
+}
+
+// One token for every sequence: four states a lane, P lanes a channel, lane = channel * P + part as the states lie in memory.  Bound by the states' bytes.
+template <typename T, int P>
+__global__ __launch_bounds__(kScanThreads) void selective_step_kernel(Selective s, uint32_t whole) {
+    constexpr int K = 4, kChannels = kScanThreads / P;
+    const uint32_t slabs = (s.channels + kChannels - 1) / kChannels, block = workgroup();
+    const uint64_t seq = block / slabs;
+    if (seq >= s.sequences) return;
+    const uint32_t ch = block % slabs * kChannels + threadIdx.x / P, n0 = threadIdx.x % P * K;
+    if (ch >= s.channels) return;                          // (all lanes of the channel)
+    const uint32_t group = ch / (s.channels / s.groups);
+    const T* const b = static_cast<const T*>(s.b.p) + seq * s.b.seq + group * s.b.group;
+    const T* const c = static_cast<const T*>(s.c.p) + seq * s.c.seq + group * s.c.group;
+    const uint64_t place = (seq * s.channels + ch) * s.states + n0;
+    float h[K], rate[K], bv[K], cv[K];
+    if (whole) {
+        const f4v v = *reinterpret_cast<const f4v*>(s.state + place), a = *reinterpret_cast<const f4v*>(s.a + (uint64_t)ch * s.states + n0);
+#pragma unroll
+        for (int k = 0; k < K; ++k) h[k] = v[k], rate[k] = a[k], bv[k] = (float)b[n0 + k], cv[k] = (float)c[n0 + k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const bool any = n0 + k < s.states;
+            h[k] = any ? s.state[place + k] : 0.0f;
+            rate[k] = any ? s.a[(uint64_t)ch * s.states + n0 + k] : 0.0f;
+            bv[k] = any ? (float)b[n0 + k] : 0.0f;
+            cv[k] = any ? (float)c[n0 + k] : 0.0f;
+        }
+    }
+    const float x = (float)static_cast<const T*>(s.x.p)[seq * s.x.seq + ch];
+    const float raw = (float)static_cast<const T*>(s.dt.p)[seq * s.dt.seq + ch] + (s.bias != nullptr ? s.bias[ch] : 0.0f);
+    const float d = s.softplus ? softplus_of(raw) : raw, u = d * x;
+    float y = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        h[k] = __builtin_fmaf(exp_of(d * rate[k]), h[k], u * bv[k]);
+        y = __builtin_fmaf(cv[k], h[k], y);
+    }
+#pragma unroll
+    for (int m = 1; m < P; m <<= 1) y += __shfl_xor(y, m);
+    if (whole) {
+        *reinterpret_cast<f4v*>(s.fin + place) = f4v{h[0], h[1], h[2], h[3]};
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (n0 + k < s.states) s.fin[place + k] = h[k];
+    }
+    if (threadIdx.x % P != 0) return;
+    if (s.skip != nullptr) y = __builtin_fmaf(s.skip[ch], x, y);
+    if (s.gate.p != nullptr) {
+        const float z = (float)static_cast<const T*>(s.gate.p)[seq * s.gate.seq + ch];
+        y *= z * sigmoid_of(z);
+    }
+    static_cast<T*>(s.out)[seq * s.out_seq + ch] = (T)y;
+}
+
+}  // namespace layers
+}  // namespace tcr

@@ -41,5 +41,48 @@ template <typename T> struct Bits;
 template <> struct Bits<_Float16> { typedef half8v v8; };
 template <> struct Bits<__bf16> { typedef bf8v v8; };
 
+constexpr int kVec = 8;                        // elements a lane loads at once: 16 bytes of 16-bit types
+
+// Vectors of kVec elements that need no more alignment than an element.
+template <typename T> struct Vec;
+template <> struct Vec<_Float16> { typedef _Float16 v __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Vec<__bf16> { typedef __bf16 v __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Vec<float> { typedef float v __attribute__((ext_vector_type(8), aligned(4))); };
+
+// The same as they are in memory.
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::v load_raw(const T* row, uint64_t col, uint64_t cols) {
+    if (col + kVec <= cols) return *reinterpret_cast<const typename Vec<T>::v*>(row + col);
+    typename Vec<T>::v x;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) x[i] = col + i < cols ? row[col + i] : (T)0.0f;
+    return x;
+}
+// Columns col .. col + 7 of a row, 0 beyond its end.
+template <typename T>
+__device__ __forceinline__ void load_vec(const T* row, uint64_t col, uint64_t cols, float (&v)[kVec]) {
+    if (col + kVec <= cols) {
+        const typename Vec<T>::v x = *reinterpret_cast<const typename Vec<T>::v*>(row + col);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = (float)x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = col + i < cols ? (float)row[col + i] : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_vec(T* row, uint64_t col, uint64_t cols, const float (&v)[kVec]) {
+    if (col + kVec <= cols) {
+        typename Vec<T>::v x;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x[i] = (T)v[i];
+        *reinterpret_cast<typename Vec<T>::v*>(row + col) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (col + i < cols) row[col + i] = (T)v[i];
+    }
+}
+
 }  // namespace layers
 }  // namespace tcr
