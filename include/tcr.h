@@ -297,6 +297,37 @@ tcr_status tcr_rms_norm_backward(const void *dout, const void *total, const void
                                  uint32_t dtype, uint32_t weight_dtype, void *stream);
 
 /*
+ * Short causal convolution of every channel with taps of its own, restarted for every sequence:
+ *   s_t = bias + sum over j < width of weight[j] x_{t-width+1+j},   out_t = s_t, or (activation == 1) s_t / (1 + exp(-s_t)).
+ * x and out hold one row of `channels` consecutive elements for every token, of the type `dtype` (TCR_F16, TCR_BF16, TCR_F32); row (sequence b, token t)
+ * starts b * stride[0] + t * stride[1] ELEMENTS behind the pointer.  weight: channels x width elements, bias: `channels` (NULL: zeros).  All of dtype; element
+ * alignment is enough.  Arithmetic is binary32, rounded once.  offsets: as in tcr_linear_attention, with 0 in rows of out whose token lies in no sequence.
+ * state, final_state: sequences x (width - 1) x channels elements, contiguous: the inputs in front of the first token and the last ones, the oldest
+ * first (with fewer tokens than width - 1 the state's own among them).  NULL: zeros, and not wanted.  They must be different arrays, and out not x.
+ * 2 <= width <= 4, channels <= 2^20, fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED beyond).  No workspace.
+ */
+typedef struct {
+    uint32_t dtype, channels, width, activation;
+    uint64_t sequences, tokens;
+    const uint64_t *offsets;
+    int64_t x_stride[2], o_stride[2];
+} tcr_convolution;
+
+tcr_status tcr_causal_conv(const tcr_convolution *shape, const void *x, const void *weight, const void *bias, void *out, const void *state, void *final_state,
+                           void *stream);
+/* One token for every sequence (tokens == 1, offsets == NULL).  new_state may be `state`. */
+tcr_status tcr_causal_conv_step(const tcr_convolution *shape, const void *x, const void *weight, const void *bias, void *out, const void *state, void *new_state,
+                                void *stream);
+/*
+ * Gradients of tcr_causal_conv.  dout is laid out by o_stride; dx is contiguous (sequence, token, channel -- packed: token, channel) and not x or dout; dweight and
+ * dbias (NULL: not wanted) like weight and bias, summed over all tokens, the same from run to run.  dfinal: the gradient of final_state (NULL: none), dstate:
+ * of `state` (NULL: not wanted; neither's array).  Takes up to 2048 / ceil(channels / 256) sums of (width + 1) * channels floats of workspace and runs with one (with less
+ * TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, as in tcr_rms_norm_backward).
+ */
+tcr_status tcr_causal_conv_backward(const tcr_convolution *shape, const void *dout, const void *x, const void *weight, const void *bias, void *dx, void *dweight,
+                                    void *dbias, const void *state, const void *dfinal, void *dstate, void *stream);
+
+/*
  * Selective state space scan: `states` running values for every channel, restarted for every sequence, whose factors depend on the data.
  *   d_t = softplus(dt_t + dt_bias)  (softplus == 0: dt_t + dt_bias),
  *   h_t[n] = exp(d_t a[n]) h_{t-1}[n] + d_t x_t b_t[n]        (binary32; h before the first token is `state`, or 0)
@@ -328,6 +359,25 @@ tcr_status tcr_selective_scan(const tcr_selective *shape, const void *x, const v
 /* One token for every sequence (tokens == 1, offsets == NULL): out and the states behind it.  new_state may be `state`. */
 tcr_status tcr_selective_scan_step(const tcr_selective *shape, const void *x, const void *dt, const void *b, const void *c, const void *gate, void *out,
                                    const float *state, float *new_state, void *stream);
+
+/*
+ * The Euclidean norm of many tensors together -- the gradients of a model -- and their scaling to a largest norm:
+ *   norm[0] = sqrt(sum of the squares of all elements),   out = min(1, max_norm / (norm + eps)) * element.
+ * tensors: `count` of them, in HOST memory (read during the call); data: DEVICE pointer to `count` consecutive elements of type dtype (TCR_F16, TCR_BF16,
+ * TCR_F32), element aligned.  norm: one float on the device.  Sums are binary64, scaled elements rounded once; results are the same from run to run.  No tensors, or
+ * empty ones: 0.  An infinity or NaN among them makes the norm infinite or NaN, and what is scaled 0 (the infinity itself NaN) or NaN.
+ * out: HOST array of `count` DEVICE pointers, where the scaled tensors go; NULL: in place.  Where the factor is 1, tensors in place are not written.  What is written
+ * stands in no other tensor's place and only once in the list (TCR_ERR_INVALID_ARG).  max_norm, eps >= 0.  At most 2^40 elements.
+ * Takes 16 KiB of workspace, or 8 bytes for each 120 tensors where that is more (with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded).
+ */
+typedef struct {
+    void *data;
+    uint64_t count;
+    uint32_t dtype;
+} tcr_tensor;
+
+tcr_status tcr_gradient_norm(const tcr_tensor *tensors, uint64_t count, float *norm, void *stream);
+tcr_status tcr_clip_gradients(const tcr_tensor *tensors, void *const *out, uint64_t count, float max_norm, float eps, float *norm, void *stream);
 
 /*
  * Bench / test hook: choose among measured alternatives.  Keys and values:

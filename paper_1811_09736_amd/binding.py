@@ -32,7 +32,9 @@ EXPORTS = (
     "tcr_set_variant", "tcr_segmented_scan_noalloc",
     "tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward",
     "tcr_rms_norm", "tcr_rms_norm_quantized", "tcr_rms_norm_backward",
+    "tcr_causal_conv", "tcr_causal_conv_step", "tcr_causal_conv_backward",
     "tcr_selective_scan", "tcr_selective_scan_step",
+    "tcr_gradient_norm", "tcr_clip_gradients",
     "tcr_kernel_name", "tcr_check_device_flags", "tcr_release", "tcr_release_stream", "tcr_status_string", "tcr_last_hip_error",
 )
 
@@ -48,11 +50,23 @@ class AttentionShape(ctypes.Structure):
         ("scale", ctypes.c_float)] + [(n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride", "o_stride")]
 
 
+class ConvolutionShape(ctypes.Structure):
+    """tcr_convolution."""
+    _fields_ = [(n, ctypes.c_uint32) for n in ("dtype", "channels", "width", "activation")] + [
+        ("sequences", ctypes.c_uint64), ("tokens", ctypes.c_uint64), ("offsets", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64 * 2) for n in ("x_stride", "o_stride")]
+
+
 class SelectiveShape(ctypes.Structure):
     """tcr_selective."""
     _fields_ = [(n, ctypes.c_uint32) for n in ("dtype", "channels", "states", "groups", "softplus")] + [
         ("sequences", ctypes.c_uint64), ("tokens", ctypes.c_uint64)] + [(n, ctypes.c_void_p) for n in ("offsets", "a", "skip", "dt_bias")] + [
         (n, ctypes.c_int64 * 2) for n in ("x_stride", "dt_stride", "gate_stride", "o_stride")] + [(n, ctypes.c_int64 * 3) for n in ("b_stride", "c_stride")]
+
+
+class TensorPlace(ctypes.Structure):
+    """tcr_tensor."""
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_uint64), ("dtype", ctypes.c_uint32)]
 
 
 class TcrError(RuntimeError):
@@ -113,10 +127,16 @@ def _load() -> ctypes.CDLL:
     for name in ("tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward", "tcr_rms_norm", "tcr_rms_norm_quantized",
                  "tcr_rms_norm_backward"):
         getattr(lib, name).restype = ctypes.c_int
-    scan = ctypes.POINTER(SelectiveShape)
+    conv, scan = ctypes.POINTER(ConvolutionShape), ctypes.POINTER(SelectiveShape)
+    lib.tcr_causal_conv.argtypes = [conv] + [vp] * 7
+    lib.tcr_causal_conv_step.argtypes = [conv] + [vp] * 7
+    lib.tcr_causal_conv_backward.argtypes = [conv] + [vp] * 11
     lib.tcr_selective_scan.argtypes = [scan] + [vp] * 9
     lib.tcr_selective_scan_step.argtypes = [scan] + [vp] * 9
-    for name in ("tcr_selective_scan", "tcr_selective_scan_step"):
+    places = ctypes.POINTER(TensorPlace)
+    lib.tcr_gradient_norm.argtypes = [places, u64, vp, vp]
+    lib.tcr_clip_gradients.argtypes = [places, ctypes.POINTER(vp), u64, f32, f32, vp, vp]
+    for name in ("tcr_gradient_norm", "tcr_clip_gradients", "tcr_causal_conv", "tcr_causal_conv_step", "tcr_causal_conv_backward", "tcr_selective_scan", "tcr_selective_scan_step"):
         getattr(lib, name).restype = ctypes.c_int
     lib.tcr_workspace_bytes.argtypes = [ctypes.c_int, u64, u64]
     lib.tcr_workspace_bytes.restype = u64
@@ -659,7 +679,7 @@ def rms_norm_backward(dout: torch.Tensor, total: torch.Tensor, weight: torch.Ten
     return dx, dweight
 
 
-# ------------------------------------------------------------------------------ selective state space scan
+# ------------------------------------------------------------------------------ short causal convolution, selective state space scan
 def _tokens_of(x, name: str, shape, dtype, like):
     """Strides of the leading dimensions of [sequence, token, ...], packed or for one token [token or sequence, ...]."""
     if not (x.is_cuda and x.dtype == dtype and x.device == like.device and tuple(x.shape) == tuple(shape) and (x.stride(-1) == 1 or x.shape[-1] == 1)):
@@ -691,6 +711,79 @@ def _token_input(x, offsets, step: bool):
     if offsets is not None:
         return _check_offsets(x, offsets), x.shape[0]
     return (x.shape[0], 1) if step else x.shape[:2]
+
+
+def _whole_of(x, name: str, shape, like) -> None:
+    if x is not None and not (x.is_cuda and x.dtype == like.dtype and x.is_contiguous() and x.device == like.device and tuple(x.shape) == tuple(shape)):
+        raise TypeError(f"{name} must be a contiguous {like.dtype} CUDA tensor of shape {tuple(shape)} on x's device")
+
+
+def _convolution(x, weight, bias, activation, offsets, out, step=False):
+    """The checked tcr_convolution of a call, and the shape of its states."""
+    sequences, tokens = _token_input(x, offsets, step)
+    channels = x.shape[-1]
+    if weight.dim() != 2 or weight.shape[1] < 2:
+        raise ValueError(f"weight has the shape {tuple(weight.shape)}; expected [channels, width]")
+    width = weight.shape[1]
+    _whole_of(weight, "weight", (channels, width), x)
+    _whole_of(bias, "bias", (channels,), x)
+    if activation not in (None, "silu"):
+        raise ValueError('activation must be None or "silu"')
+    rows = [_two(_tokens_of(t, name, x.shape, x.dtype, x), offsets is not None, step, 1) for t, name in ((x, "x"), (out, "out"))]
+    return (ConvolutionShape(_DTYPES[x.dtype], channels, width, 0 if activation is None else 1, sequences, tokens, _ptr(offsets), *rows),
+            (sequences, width - 1, channels))
+
+
+def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: Optional[str] = "silu",
+                offsets: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None, final_state: bool = False,
+                out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """tcr_causal_conv: every channel's inputs with its `width` taps, the last of them at the token itself, and silu.
+
+    x [B, T, D], or packed sequences [M, D] with `offsets` ([sequences + 1], int64); weight [D, width], bias [D] (2 <= width <= 4); activation "silu" or
+    None.  state [sequences, width - 1, D]: the inputs in front of the first tokens, the oldest first.  All of x's type.  Returns out like x (a given one
+    not x), with final_state also the last width - 1 inputs of every sequence."""
+    given = out
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    shape, states = _convolution(x, weight, bias, activation, offsets, out)
+    _whole_of(state, "state", states, x)
+    last = torch.empty(states, dtype=x.dtype, device=x.device) if final_state else None
+    _run(_lib.tcr_causal_conv, "tcr_causal_conv", x, stream, shape, x.data_ptr(), weight.data_ptr(), _ptr(bias), out.data_ptr(), _ptr(state), _ptr(last))
+    _written(given)
+    return (out, last) if final_state else out
+
+
+def causal_conv_step(x: torch.Tensor, weight: torch.Tensor, state: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: Optional[str] = "silu",
+                     new_state: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """tcr_causal_conv_step: one token for every sequence.  x [B, D], state [B, width - 1, D].  The new states go to new_state, without it to `state`
+    itself.  Returns out [B, D]."""
+    given = out
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    shape, states = _convolution(x, weight, bias, activation, None, out, step=True)
+    if new_state is None:
+        new_state = state
+    for t, name in ((state, "state"), (new_state, "new_state")):
+        _whole_of(t, name, states, x)
+    _run(_lib.tcr_causal_conv_step, "tcr_causal_conv_step", x, stream, shape, x.data_ptr(), weight.data_ptr(), _ptr(bias), out.data_ptr(), state.data_ptr(),
+         new_state.data_ptr())
+    _written(new_state, given)
+    return out
+
+
+def causal_conv_backward(dout: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                         activation: Optional[str] = "silu", offsets: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None,
+                         dfinal: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """tcr_causal_conv_backward: (dx, dweight, dbias, dstate) from dout and, where the final states were used, their gradient dfinal.  dbias is None
+    without a bias, dstate without `state`."""
+    shape, states = _convolution(x, weight, bias, activation, offsets, dout)
+    _whole_of(state, "state", states, x)
+    _whole_of(dfinal, "dfinal", states, x)
+    dx, dweight, dbias, dstate = (None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (x, weight, bias, state))
+    _run(_lib.tcr_causal_conv_backward, "tcr_causal_conv_backward", x, stream, shape, dout.data_ptr(), x.data_ptr(), weight.data_ptr(), _ptr(bias),
+         dx.data_ptr(), dweight.data_ptr(), _ptr(dbias), _ptr(state), _ptr(dfinal), _ptr(dstate))
+    return dx, dweight, dbias, dstate
 
 
 def _selective(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, out, step=False):
@@ -753,6 +846,67 @@ def selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: t
          out.data_ptr(), state.data_ptr(), new_state.data_ptr())
     _written(new_state, given)
     return out
+
+
+# ------------------------------------------------------------------------------ norm over many tensors, clipping
+def _fills_memory(x: torch.Tensor) -> bool:
+    """Whether x's elements are consecutive in some order of its dimensions, each once."""
+    if x.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted(zip(x.stride(), x.shape)):
+        if size == 1:
+            continue
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+def _places(tensors):
+    """The tensors as a list, and as an array of tcr_tensor."""
+    tensors = [tensors] if isinstance(tensors, torch.Tensor) else list(tensors)
+    places = (TensorPlace * len(tensors))()
+    for place, t in zip(places, tensors):
+        if not (t.is_cuda and t.dtype in (torch.float16, torch.bfloat16, torch.float32) and t.device == tensors[0].device and _fills_memory(t)):
+            raise TypeError("tensors must be float16, bfloat16 or float32 CUDA tensors of one device whose elements are consecutive")
+        place.data, place.count, place.dtype = t.data_ptr(), t.numel(), _DTYPES[t.dtype]
+    return tensors, places
+
+
+def _norm_of(tensors) -> torch.Tensor:
+    return torch.empty((), dtype=torch.float32, device=tensors[0].device if tensors else "cuda")
+
+
+def gradient_norm(tensors, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """tcr_gradient_norm: the Euclidean norm of all the tensors' elements together, a float32 tensor without dimensions."""
+    tensors, places = _places(tensors)
+    norm = _norm_of(tensors)
+    _run(_lib.tcr_gradient_norm, "tcr_gradient_norm", norm, stream, places, len(tensors), norm.data_ptr())
+    return norm
+
+
+def clip_gradients(tensors, max_norm: float, eps: float = 1e-6, out=None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """tcr_clip_gradients: scales the tensors by min(1, max_norm / (norm + eps)), in place, or to the tensors `out` of the same types, shapes and strides.
+    Returns their norm in front of it, a float32 tensor without dimensions.  No tensor may stand twice in the list."""
+    tensors, places = _places(tensors)
+    to = None
+    if out is not None:
+        out = [out] if isinstance(out, torch.Tensor) else list(out)
+        if len(out) != len(tensors):
+            raise ValueError(f"out holds {len(out)} tensors for {len(tensors)}")
+        for t, o in zip(tensors, out):
+            if not (o.is_cuda and o.dtype == t.dtype and o.device == t.device and o.shape == t.shape and _same_layout(t, o)):
+                raise TypeError("out must hold a CUDA tensor of the type, shape, strides and device of each tensor")
+        to = (ctypes.c_void_p * len(out))(*(o.data_ptr() for o in out))
+    norm = _norm_of(tensors)
+    _run(_lib.tcr_clip_gradients, "tcr_clip_gradients", norm, stream, places, to, len(tensors), max_norm, eps, norm.data_ptr())
+    _written(*(tensors if out is None else out))
+    return norm
+
+
+def _same_layout(x: torch.Tensor, y: torch.Tensor) -> bool:
+    return x.stride() == y.stride() or (x.is_contiguous() and y.is_contiguous())
 
 
 def workspace_bytes(op: int, n: int, seg_len: int) -> int:

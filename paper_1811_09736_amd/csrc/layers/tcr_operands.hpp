@@ -1,6 +1,7 @@
 // Checks on the arrays of a call that the host sides of the scan and the convolution share.
 #pragma once
 #include <exception>
+#include <type_traits>
 
 #include "tcr_shared.hpp"
 

@@ -8,7 +8,7 @@
 // whole chunk; what a token needs of its channel (d and d x) and of its group (b, c) stands in LDS as binary32, made once by whole vectors.
 // What bounds it is the vector unit: an exponential (3.2 times a multiply-add), two multiplications and two multiply-adds for each state.
 #pragma once
-#include "tcr_shared.hpp"
+#include "tcr_places.hpp"
 
 namespace tcr {
 namespace layers {
@@ -35,8 +35,6 @@ struct Selective {
     uint32_t softplus;
 };
 
-constexpr float kLog2e = 1.44269504088896340736f;
-
 // log(1 + e) for e in [0, 1] as 2 atanh(e / (2 + e)); the series ends at s^17, s <= 1/3: 2 s^19 / 19 < 2^-32 of it.  Two roundings more than
 // the sum's own, and none of it lost where e is small.
 __device__ __forceinline__ float log1p_unit(float e) {
@@ -52,57 +50,7 @@ __device__ __forceinline__ float log1p_unit(float e) {
     v = __builtin_fmaf(v, q, 2.0f / 3.0f);
     return __builtin_fmaf(s * q, v, 2.0f * s);
 }
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ __forceinline__ float softplus_of(float x) { return (x > 0.0f ? x : 0.0f) + log1p_unit(exp_of(-__builtin_fabsf(x))); }
-// 1 / (1 + exp(-x)): from 0 at minus infinity to 1.
-__device__ __forceinline__ float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }
-
-// Where the sequences of a span begin and end.  bound(i) never leaves the span, whatever the offsets hold.
-struct Bounds {
-    const uint64_t* offsets;
-    uint32_t count, span;
-    __device__ __forceinline__ uint32_t at(uint32_t i) const {
-        const uint64_t o = offsets[i];
-        return o < span ? (uint32_t)o : span;
-    }
-    // How many of the count + 1 bounds are at most t.
-    __device__ __forceinline__ uint32_t upto(uint32_t t) const {
-        uint32_t low = 0, high = count + 1;
-        while (low < high) {
-            const uint32_t mid = low + (high - low) / 2;
-            if (at(mid) <= t) low = mid + 1;
-            else high = mid;
-        }
-        return low;
-    }
-};
-
-// The sequence that a token of a span stands in, and where the next bound is.
-struct Place {
-    uint32_t seq, next;                        // next: the first bound behind the token (none: ~0)
-    uint32_t start;
-    bool inside;
-    __device__ __forceinline__ void find(const Bounds& b, uint32_t span_index, uint32_t t) {
-        if (b.offsets == nullptr) {
-            seq = span_index, start = 0, next = b.span, inside = true;
-            return;
-        }
-        const uint32_t n = b.upto(t);
-        inside = n >= 1 && n <= b.count;
-        seq = n - 1;
-        start = inside ? b.at(seq) : 0;
-        next = n <= b.count ? b.at(n) : ~0u;
-    }
-    // Over the bound at t, and over empty sequences there.
-    __device__ __forceinline__ void pass(const Bounds& b, uint32_t t) {
-        do ++seq;
-        while (seq < b.count && b.at(seq + 1) <= t);
-        inside = seq < b.count;
-        start = t;
-        next = inside ? b.at(seq + 1) : ~0u;
-    }
-};
-
 // The states n0 .. n0 + K - 1 of a channel in an array [sequence][channel][state]; 0 where there is no array or no such state.
 template <int K>
 __device__ __forceinline__ void load_states(const float* states, uint64_t seq, const Selective& s, uint32_t ch, uint32_t n0, bool real, float (&h)[K]) {
