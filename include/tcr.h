@@ -361,6 +361,17 @@ tcr_status tcr_selective_scan_step(const tcr_selective *shape, const void *x, co
                                    const float *state, float *new_state, void *stream);
 
 /*
+ * Gradients of tcr_selective_scan.  dout is laid out by o_stride; dx, ddt, dgate (NULL where gate is) are contiguous (sequence, token, channel -- packed: token, channel),
+ * db and dc (sequence, token, group, state), summed over a group's channels; da, dskip, ddt_bias (NULL: not wanted) like a, skip and dt_bias, summed over all tokens: the
+ * same from run to run.  None of them stands in an input's place (not checked but for dstate).  state: the forward call's; dfinal: the gradient of its final_state (NULL: none);
+ * dstate: the gradient of `state` (NULL: not wanted).  With p the power of two from 4 to 64 that holds the states, workspace of about tokens * channels * (4 + p * p / 128) bytes
+ * -- 6 for 16 states -- and 12 * channels for each sequence; with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, and nothing done.
+ */
+tcr_status tcr_selective_scan_backward(const tcr_selective *shape, const void *dout, const void *x, const void *dt, const void *b, const void *c,
+                                       const void *gate, void *dx, void *ddt, float *da, void *db, void *dc, float *dskip, void *dgate, float *ddt_bias,
+                                       const float *state, const float *dfinal, float *dstate, void *stream);
+
+/*
  * The Euclidean norm of many tensors together -- the gradients of a model -- and their scaling to a largest norm:
  *   norm[0] = sqrt(sum of the squares of all elements),   out = min(1, max_norm / (norm + eps)) * element.
  * tensors: `count` of them, in HOST memory (read during the call); data: DEVICE pointer to `count` consecutive elements of type dtype (TCR_F16, TCR_BF16,

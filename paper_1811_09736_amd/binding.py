@@ -33,7 +33,7 @@ EXPORTS = (
     "tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward",
     "tcr_rms_norm", "tcr_rms_norm_quantized", "tcr_rms_norm_backward",
     "tcr_causal_conv", "tcr_causal_conv_step", "tcr_causal_conv_backward",
-    "tcr_selective_scan", "tcr_selective_scan_step",
+    "tcr_selective_scan", "tcr_selective_scan_step", "tcr_selective_scan_backward",
     "tcr_gradient_norm", "tcr_clip_gradients",
     "tcr_kernel_name", "tcr_check_device_flags", "tcr_release", "tcr_release_stream", "tcr_status_string", "tcr_last_hip_error",
 )
@@ -133,10 +133,12 @@ def _load() -> ctypes.CDLL:
     lib.tcr_causal_conv_backward.argtypes = [conv] + [vp] * 11
     lib.tcr_selective_scan.argtypes = [scan] + [vp] * 9
     lib.tcr_selective_scan_step.argtypes = [scan] + [vp] * 9
+    lib.tcr_selective_scan_backward.argtypes = [scan] + [vp] * 18
     places = ctypes.POINTER(TensorPlace)
     lib.tcr_gradient_norm.argtypes = [places, u64, vp, vp]
     lib.tcr_clip_gradients.argtypes = [places, ctypes.POINTER(vp), u64, f32, f32, vp, vp]
-    for name in ("tcr_gradient_norm", "tcr_clip_gradients", "tcr_causal_conv", "tcr_causal_conv_step", "tcr_causal_conv_backward", "tcr_selective_scan", "tcr_selective_scan_step"):
+    for name in ("tcr_gradient_norm", "tcr_clip_gradients", "tcr_causal_conv", "tcr_causal_conv_step", "tcr_causal_conv_backward", "tcr_selective_scan", "tcr_selective_scan_step",
+                 "tcr_selective_scan_backward"):
         getattr(lib, name).restype = ctypes.c_int
     lib.tcr_workspace_bytes.argtypes = [ctypes.c_int, u64, u64]
     lib.tcr_workspace_bytes.restype = u64
@@ -846,6 +848,24 @@ def selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: t
          out.data_ptr(), state.data_ptr(), new_state.data_ptr())
     _written(new_state, given)
     return out
+
+
+def selective_scan_backward(dout: torch.Tensor, x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor,
+                            skip: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None,
+                            softplus: bool = True, offsets: Optional[torch.Tensor] = None, state: Optional[torch.Tensor] = None,
+                            dfinal: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """tcr_selective_scan_backward: (dx, ddt, da, db, dc, dskip, dgate, ddt_bias, dstate) from dout and, where the final states were used, their gradient
+    dfinal.  None in the place of what was not given: skip, gate, dt_bias, state."""
+    shape = _selective(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, dout)
+    states = (shape.sequences, shape.channels, shape.states)
+    _constants_of(state, "state", states, x)
+    _constants_of(dfinal, "dfinal", states, x)
+    dx, ddt, da, db, dc, dskip, dgate, dbias, dstate = (
+        None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (x, dt, a, b, c, skip, gate, dt_bias, state))
+    _run(_lib.tcr_selective_scan_backward, "tcr_selective_scan_backward", x, stream, shape, dout.data_ptr(), x.data_ptr(), dt.data_ptr(), b.data_ptr(),
+         c.data_ptr(), _ptr(gate), dx.data_ptr(), ddt.data_ptr(), da.data_ptr(), db.data_ptr(), dc.data_ptr(), _ptr(dskip), _ptr(dgate), _ptr(dbias),
+         _ptr(state), _ptr(dfinal), _ptr(dstate))
+    return dx, ddt, da, db, dc, dskip, dgate, dbias, dstate
 
 
 # ------------------------------------------------------------------------------ norm over many tensors, clipping

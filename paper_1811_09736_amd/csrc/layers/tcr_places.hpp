@@ -34,8 +34,8 @@ struct Bounds {
 // The sequence that a token of a span stands in, and where the next bound is.
 struct Place {
     uint32_t seq, next;                        // next: the first bound behind the token (none: ~0)
-    uint32_t start;
-    bool inside;
+    uint32_t start;                            // the last bound that is not behind it (none: 0)
+    bool inside;                               // whether it stands in a sequence at all
     __device__ __forceinline__ void find(const Bounds& b, uint32_t span_index, uint32_t t) {
         if (b.offsets == nullptr) {
             seq = span_index, start = 0, next = b.span, inside = true;
@@ -44,7 +44,7 @@ struct Place {
         const uint32_t n = b.upto(t);
         inside = n >= 1 && n <= b.count;
         seq = n - 1;
-        start = inside ? b.at(seq) : 0;
+        start = n >= 1 ? b.at(n - 1) : 0;
         next = n <= b.count ? b.at(n) : ~0u;
     }
     // Over the bound at t, and over empty sequences there.
