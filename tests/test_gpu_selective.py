@@ -1,0 +1,376 @@
+"""The selective scan against its definition in 64 bits: prompts, packed sequences, single tokens, gradients.
+
+Tolerances.  The kernels compute in binary32 and round once to the type of the outputs: half a step of it, eps / 2 of the value.  In front of that, every value is a sum of
+products; each product passes a bounded number of roundings for each token it is carried over (the factor's argument and exponential, the carried product, the addition: eight, with
+the exponent's own size for its argument's relative error) and for the sums it enters (states, channels, tokens).  So the error of a result is at most
+(8 tokens + terms) 2^-24 times the same sum with every term's magnitude, which the reference computes beside it (`large`): a bound that holds for every order of additions.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+UNIT = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def tcr():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1811_09736_amd import binding
+    yield binding
+    binding.check_device_flags()
+
+
+def sequences_of(x, offsets):
+    """(index, length) of every sequence in [B, T, ...] or packed [M, ...]."""
+    if offsets is None:
+        return [((i, slice(None)), x.shape[1]) for i in range(x.shape[0])]
+    o = offsets.tolist()
+    return [((slice(o[i], o[i + 1]),), o[i + 1] - o[i]) for i in range(len(o) - 1)]
+
+
+def reference(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, state, dout=None, dfinal=None, large=False):
+    """The definition, token by token.  Without dout (out, last states), with it the gradients by name.  large: with every term's magnitude."""
+    size = (lambda v: v.abs()) if large else (lambda v: v)
+    x, dt, b, c = (v.double() for v in (x, dt, b, c))
+    gate, dout, state, dfinal = (None if v is None else v.double() for v in (gate, dout, state, dfinal))
+    rate = a.double()
+    channels, n = rate.shape
+    each = channels // b.shape[-2]
+    raw = dt if dt_bias is None else dt + dt_bias.double()
+    d = torch.where(raw > 40, raw, torch.log1p(torch.exp(raw.clamp(max=40)))) if softplus else raw
+    sk = torch.zeros(channels, device=x.device, dtype=torch.float64) if skip is None else skip.double()
+    g = torch.ones_like(x) if gate is None else gate / (1 + torch.exp(-gate))
+    count = len(sequences_of(x, offsets))
+    out = torch.zeros_like(x)
+    last = torch.zeros(count, channels, n, device=x.device, dtype=torch.float64)
+    grads = {k: torch.zeros_like(v) for k, v in (("dx", x), ("ddt", x), ("da", rate), ("db", b), ("dc", b), ("dskip", sk), ("dgate", x), ("dbias", sk), ("dstate", last))}
+    for i, (at, length) in enumerate(sequences_of(x, offsets)):
+        h = size(state[i]) if state is not None else torch.zeros_like(last[i])
+        xs, ds, gs = size(x[at]), d[at], size(g[at])
+        bs, cs = (size(v[at]).repeat_interleave(each, 1) for v in (b, c))
+        keep = torch.exp(ds[..., None] * rate)
+        ds = size(ds)
+        hs = [h]
+        for t in range(length):
+            h = keep[t] * h + (ds[t] * xs[t])[:, None] * bs[t]
+            hs.append(h)
+        y = torch.stack([(cs[t] * hs[t + 1]).sum(1) for t in range(length)]) + size(sk) * xs if length else torch.zeros_like(xs)
+        out[at], last[i] = y * gs, h
+        if dout is None:
+            continue
+        dys = size(dout[at]) * gs
+        if gate is not None:
+            s = 1 / (1 + torch.exp(-gate[at]))
+            # (a sum of two terms, each rounded by itself, that cancel near gate = -1.28: their magnitudes count, as everywhere)
+            grads["dgate"][at] = size(dout[at]) * y * (s + size(gate[at]) * s * (1 - s))
+        back = size(dfinal[i]) if dfinal is not None else torch.zeros_like(last[i])
+        for t in range(length - 1, -1, -1):
+            grad = cs[t] * dys[t][:, None] + back
+            through = grad * keep[t] * hs[t]
+            gb = (grad * bs[t]).sum(1)
+            grads["dx"][at][t] = gb * ds[t] + size(sk) * dys[t]
+            grads["ddt"][at][t] = gb * xs[t] + (through * size(rate)).sum(1)
+            grads["da"] += through * ds[t][:, None]
+            grads["db"][at][t] = (grad * (ds[t] * xs[t])[:, None]).unflatten(0, (-1, each)).sum(1)
+            grads["dc"][at][t] = (dys[t][:, None] * hs[t + 1]).unflatten(0, (-1, each)).sum(1)
+            back = grad * keep[t]
+        grads["dstate"][i] = back
+        grads["dskip"] += (dys * xs).sum(0)
+        if softplus:
+            grads["ddt"][at] *= 1 / (1 + torch.exp(-raw[at]))
+        grads["dbias"] += grads["ddt"][at].sum(0)
+    return (out, last) if dout is None else grads
+
+
+def make(dtype, lead, channels, states, groups=1, gate=True, skip=True, bias=True, state=None, seed=0, poison=None):
+    """Inputs as parts of wider rows, so that strides differ and rows begin at odd elements."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    both = rand(*lead, 2 * channels + 3).to(dtype)
+    rest = rand(*lead, channels + 2 * groups * states + 1).to(dtype)
+    if poison is not None:
+        both[poison], rest[poison] = float("nan"), float("nan")
+    x, z = both[..., 1:channels + 1], both[..., channels + 2:2 * channels + 2]
+    dt = rest[..., :channels]
+    b, c = (v.unflatten(-1, (groups, states)) for v in rest[..., channels:channels + 2 * groups * states].chunk(2, -1))
+    return {"x": x, "dt": dt, "a": -torch.rand(channels, states, generator=gen, device="cuda") * 4, "b": b, "c": c, "skip": rand(channels) if skip else None,
+            "gate": z if gate else None, "dt_bias": rand(channels) - 2 if bias else None, "state": rand(state, channels, states) if state else None}
+
+
+def worst(got, want, large, terms):
+    """The largest error as a multiple of what the bound allows."""
+    half = 0.0 if got.dtype == torch.float32 else torch.finfo(got.dtype).eps / 2
+    tiny = {torch.float32: 2.0 ** -126, torch.bfloat16: 2.0 ** -126, torch.float16: 2.0 ** -25}[got.dtype]
+    room = terms * UNIT * large + half * (want.abs() + terms * UNIT * large) + tiny
+    if got.numel() == 0:
+        return 0.0
+    off = (got.double() - want).abs()
+    assert torch.isfinite(off).all()
+    return float((off / room).max())
+
+
+def check(got, want, large, terms, name):
+    assert got.shape == want.shape, name
+    times = worst(got, want, large, terms)
+    assert times <= 1.0, f"{name}: {times} times the bound"
+
+
+GAPS = [3, 3, 10, 11, 11, 11, 97, 130, 130, 257, 300]        # of 311 tokens: nothing in front of 3 and behind 300, empty sequences, one of a single token
+DENSE = [  # type, lead, channels, states, groups
+    (torch.float32, (1, 1), 1, 1, 1), (torch.float32, (2, 5), 3, 2, 1), (torch.bfloat16, (3, 33), 64, 16, 1), (torch.float16, (1, 300), 70, 16, 1),
+    (torch.float32, (2, 129), 96, 8, 2), (torch.bfloat16, (1, 257), 40, 64, 1), (torch.float16, (2, 100), 130, 5, 2), (torch.float32, (1, 260), 33, 33, 1),
+    (torch.bfloat16, (1, 70), 300, 3, 3), (torch.float32, (70, 4), 17, 16, 1), (torch.float32, (1, 700), 8, 20, 1)]
+
+
+@pytest.mark.parametrize("dtype,lead,channels,states,groups", DENSE, ids=str)
+@pytest.mark.parametrize("whole", [True, False], ids=["whole", "bare"])
+def test_prompts(tcr, dtype, lead, channels, states, groups, whole):
+    v = make(dtype, lead, channels, states, groups, gate=whole, skip=whole, bias=whole, state=lead[0] if whole else None)
+    out, last = tcr.selective_scan(v["x"], v["dt"], v["a"], v["b"], v["c"], skip=v["skip"], gate=v["gate"], dt_bias=v["dt_bias"], state=v["state"], final_state=True)
+    want, large = (reference(**v, softplus=True, offsets=None, large=m) for m in (False, True))
+    terms = 8 * lead[1] + states + 16
+    check(out, want[0], large[0], terms, "out")
+    check(last, want[1], large[1], terms, "states")
+
+
+@pytest.mark.parametrize("dtype,channels,states,groups", [(torch.float32, 70, 16, 1), (torch.bfloat16, 64, 8, 2), (torch.float16, 33, 3, 1), (torch.float32, 20, 64, 2),
+                                                          (torch.bfloat16, 520, 32, 1)], ids=str)
+@pytest.mark.parametrize("state", [True, False], ids=["state", "none"])
+def test_packed(tcr, dtype, channels, states, groups, state):
+    poison = torch.ones(311, dtype=torch.bool, device="cuda")
+    poison[3:300] = False                    # NaN where no sequence is
+    v = make(dtype, (311,), channels, states, groups, state=10 if state else None, poison=poison)
+    offsets = torch.tensor(GAPS, device="cuda")
+    out, last = tcr.selective_scan(v["x"], v["dt"], v["a"], v["b"], v["c"], skip=v["skip"], gate=v["gate"], dt_bias=v["dt_bias"], offsets=offsets, state=v["state"],
+                                   final_state=True)
+    assert (out[:3] == 0).all() and (out[300:] == 0).all()
+    want, large = (reference(**v, softplus=True, offsets=offsets, large=m) for m in (False, True))
+    terms = 8 * 127 + states + 16
+    check(out, want[0], large[0], terms, "out")
+    check(last, want[1], large[1], terms, "states")
+    if state:
+        assert torch.equal(last[0], v["state"][0]) and torch.equal(last[3], v["state"][3])       # empty sequences
+
+
+def test_packed_alone_and_not_at_all(tcr):
+    v = make(torch.float32, (40,), 20, 16, state=3)
+    args, given = (v["x"], v["dt"], v["a"], v["b"], v["c"]), {k: v[k] for k in ("skip", "gate", "dt_bias", "state")}
+    for bounds in ([0, 0, 0, 0], [40, 40, 40, 40], [0, 40, 40, 40], [0, 0, 0, 40]):
+        offsets = torch.tensor(bounds, device="cuda")
+        out, last = tcr.selective_scan(*args, **given, offsets=offsets, final_state=True)
+        want, large = (reference(**v, softplus=True, offsets=offsets, large=m) for m in (False, True))
+        check(out, want[0], large[0], 8 * 40 + 32, str(bounds))
+        check(last, want[1], large[1], 8 * 40 + 32, str(bounds))
+
+
+@pytest.mark.parametrize("empty", [(0, 5), (3, 0), (0, 0)], ids=str)
+def test_nothing(tcr, empty):
+    v = make(torch.bfloat16, empty, 24, 16, state=empty[0])
+    out, last = tcr.selective_scan(v["x"], v["dt"], v["a"], v["b"], v["c"], skip=v["skip"], gate=v["gate"], state=v["state"], final_state=True)
+    assert out.shape == (*empty, 24) and torch.equal(last, v["state"] if v["state"] is not None else last)
+    got = tcr.selective_scan_backward(torch.zeros_like(out), v["x"], v["dt"], v["a"], v["b"], v["c"], skip=v["skip"], gate=v["gate"], state=v["state"],
+                                      dfinal=None if v["state"] is None else v["state"] * 2)
+    assert (got[2] == 0).all() and (got[5] == 0).all()
+    if v["state"] is not None:
+        assert torch.equal(got[8], v["state"] * 2)
+
+
+@pytest.mark.parametrize("raw", [True, False], ids=["raw", "softplus"])
+def test_steps_of_all_sizes(tcr, raw):
+    """d from 0 to hundreds, and negative ones without the softplus; rates of both signs and zero."""
+    x = torch.randn(1, 64, 16, device="cuda")
+    dt = torch.linspace(-90, 90, 64, device="cuda")[None, :, None].expand(1, 64, 16).contiguous() * (0.01 if raw else 1.0)
+    a = torch.cat([torch.zeros(16, 1, device="cuda"), -torch.rand(16, 2, device="cuda") * 3, torch.rand(16, 1, device="cuda") * 1e-3], 1)
+    b, c = torch.randn(1, 64, 1, 4, device="cuda"), torch.randn(1, 64, 1, 4, device="cuda")
+    got = tcr.selective_scan(x, dt, a, b, c, softplus=not raw, final_state=True)
+    want, large = (reference(x, dt, a, b, c, None, None, None, not raw, None, None, large=m) for m in (False, True))
+    # (exponents of up to 270 here: their argument's own rounding counts as often)
+    for g, w, m in zip(got, want, large):
+        check(g, w, m, 64 * (8 + 300), "values")
+
+
+def test_step_goes_on_like_the_prompt(tcr):
+    for dtype, channels, states, groups in ((torch.float32, 70, 16, 1), (torch.bfloat16, 64, 7, 2), (torch.float16, 33, 64, 1), (torch.float32, 5, 1, 1), (torch.bfloat16, 600, 24, 1)):
+        v = make(dtype, (5, 9), channels, states, groups, state=5)
+        given = {k: v[k] for k in ("skip", "gate", "dt_bias")}
+        want, large = (reference(**v, softplus=True, offsets=None, large=m) for m in (False, True))
+        state = v["state"].clone()
+        for t in range(9):
+            now = {k: None if g is None else g[:, t] for k, g in given.items() if k == "gate"}
+            other = torch.empty_like(state)
+            got = tcr.selective_scan_step(v["x"][:, t], v["dt"][:, t], v["a"], v["b"][:, t], v["c"][:, t], state, skip=v["skip"], dt_bias=v["dt_bias"], new_state=other, **now)
+            same = tcr.selective_scan_step(v["x"][:, t], v["dt"][:, t], v["a"], v["b"][:, t], v["c"][:, t], state, skip=v["skip"], dt_bias=v["dt_bias"], **now)
+            assert torch.equal(state, other) and torch.equal(got, same)
+            check(got, want[0][:, t], large[0][:, t], 8 * 9 + states + 16, "out")
+        check(state, want[1], large[1], 8 * 9 + 16, "states")
+
+
+def grads_of(tcr, v, dout, offsets, dfinal, softplus=True):
+    got = tcr.selective_scan_backward(dout, v["x"], v["dt"], v["a"], v["b"], v["c"], skip=v["skip"], gate=v["gate"], dt_bias=v["dt_bias"], softplus=softplus, offsets=offsets,
+                                      state=v["state"], dfinal=dfinal)
+    return dict(zip(("dx", "ddt", "da", "db", "dc", "dskip", "dgate", "dbias", "dstate"), got))
+
+
+def check_grads(got, want, large, longest, tokens, v):
+    channels, states = v["a"].shape
+    each = channels // v["b"].shape[-2]
+    # (carried forwards and backwards, then summed over channels or over all tokens)
+    base = 16 * longest + states + 32
+    for name, g in got.items():
+        if g is None:
+            continue
+        terms = base + (each if name in ("db", "dc") else tokens if name in ("da", "dskip", "dbias") else 0)
+        check(g, want[name], large[name], terms, name)
+
+
+@pytest.mark.parametrize("dtype,lead,channels,states,groups", DENSE, ids=str)
+@pytest.mark.parametrize("whole", [True, False], ids=["whole", "bare"])
+def test_gradients(tcr, dtype, lead, channels, states, groups, whole):
+    v = make(dtype, lead, channels, states, groups, gate=whole, skip=whole, bias=whole, state=lead[0] if whole else None, seed=3)
+    dout = torch.randn(*lead, channels + 2, device="cuda").to(dtype)[..., 1:-1]
+    dfinal = torch.randn(lead[0], channels, states, device="cuda") if whole else None
+    got = grads_of(tcr, v, dout, None, dfinal)
+    assert [k for k in got if got[k] is None] == ([] if whole else ["dskip", "dgate", "dbias", "dstate"])
+    want, large = (reference(**v, softplus=True, offsets=None, dout=dout, dfinal=dfinal, large=m) for m in (False, True))
+    check_grads(got, want, large, lead[1], lead[0] * lead[1], v)
+
+
+@pytest.mark.parametrize("dtype,channels,states,groups", [(torch.float32, 70, 16, 1), (torch.bfloat16, 64, 8, 2), (torch.float16, 33, 3, 1), (torch.float32, 20, 64, 2),
+                                                          (torch.bfloat16, 300, 32, 1)], ids=str)
+@pytest.mark.parametrize("state,final", [(True, True), (True, False), (False, True), (False, False)], ids=str)
+def test_gradients_packed(tcr, dtype, channels, states, groups, state, final):
+    poison = torch.ones(311, dtype=torch.bool, device="cuda")
+    poison[3:300] = False
+    v = make(dtype, (311,), channels, states, groups, state=10 if state else None, poison=poison, seed=4)
+    offsets = torch.tensor(GAPS, device="cuda")
+    dout = torch.randn(311, channels, device="cuda").to(dtype)
+    dout[poison] = float("nan")
+    dfinal = torch.randn(10, channels, states, device="cuda") if final else None
+    got = grads_of(tcr, v, dout, offsets, dfinal)
+    for name in ("dx", "ddt", "db", "dc", "dgate"):
+        assert (got[name][poison] == 0).all(), name
+    want, large = (reference(**v, softplus=True, offsets=offsets, dout=dout, dfinal=dfinal, large=m) for m in (False, True))
+    check_grads(got, want, large, 127, 297, v)
+    if state and final:
+        assert torch.equal(got["dstate"][0], dfinal[0])
+
+
+def test_gradients_without_softplus(tcr):
+    v = make(torch.float32, (2, 50), 24, 16, state=2, seed=5)
+    v["dt"] = (v["dt"] * 0.2).contiguous()
+    v["dt_bias"] = v["dt_bias"] * 0.05
+    dout, dfinal = torch.randn(2, 50, 24, device="cuda"), torch.randn(2, 24, 16, device="cuda")
+    got = grads_of(tcr, v, dout, None, dfinal, softplus=False)
+    want, large = (reference(**v, softplus=False, offsets=None, dout=dout, dfinal=dfinal, large=m) for m in (False, True))
+    check_grads(got, want, large, 50, 100, v)
+
+
+def test_gradients_against_differences(tcr):
+    """Along a random direction of all inputs: central differences of the definition in 64 bits, h = 2^-13, whose own error is h^2 / 6 of a third derivative (of the order of the
+    loss itself for inputs and rates of the order of 1: 2^-28) and 2^-52 / h of the loss's rounding."""
+    v = make(torch.float32, (2, 40), 12, 8, groups=2, state=2, seed=6)
+    names = ["x", "dt", "a", "b", "c", "skip", "gate", "dt_bias", "state"]
+    dout, dfinal = torch.randn(2, 40, 12, device="cuda"), torch.randn(2, 12, 8, device="cuda")
+    got = grads_of(tcr, v, dout, None, dfinal)
+    way = {n: torch.randn_like(v[n]).double() for n in names}
+
+    def loss(step):
+        out, last = reference(**{n: v[n].double() + step * way[n] for n in names}, softplus=True, offsets=None)
+        return float((out * dout.double()).sum() + (last * dfinal.double()).sum())
+
+    h = 2.0 ** -13
+    slope = (loss(h) - loss(-h)) / (2 * h)
+    of = dict(zip(names, ("dx", "ddt", "da", "db", "dc", "dskip", "dgate", "dbias", "dstate")))
+    terms = [(got[of[n]].double() * way[n]) for n in names]
+    size = math.sqrt(sum(float((t * t).sum()) for t in terms))
+    assert abs(slope - sum(float(t.sum()) for t in terms)) <= 1e-4 * size
+
+
+def test_infinities_stay_where_they_are(tcr):
+    v = make(torch.float32, (60,), 20, 16, state=3, seed=7)
+    offsets = torch.tensor([0, 20, 40, 60], device="cuda")
+    args = lambda: (v["x"], v["dt"], v["a"], v["b"], v["c"])  # noqa: E731
+    given = {k: v[k] for k in ("skip", "gate", "dt_bias", "state")}
+    clean = tcr.selective_scan(*args(), **given, offsets=offsets, final_state=True)
+    v["x"] = v["x"].clone()
+    v["x"][25, 4], v["x"][30, 5] = float("inf"), float("nan")
+    out, last = tcr.selective_scan(*args(), **given, offsets=offsets, final_state=True)
+    hit = torch.zeros(60, 20, dtype=torch.bool, device="cuda")
+    hit[25:40, 4], hit[30:40, 5] = True, True
+    assert torch.equal(out[~hit], clean[0][~hit]) and not torch.isfinite(out[hit]).any()
+    lost = torch.zeros(3, 20, dtype=torch.bool, device="cuda")
+    lost[1, 4:6] = True
+    assert torch.equal(last[~lost], clean[1][~lost])
+
+
+def test_same_from_run_to_run(tcr):
+    v = make(torch.bfloat16, (2, 500), 200, 16, state=2, seed=8)
+    dout = torch.randn(2, 500, 200, device="cuda").to(torch.bfloat16)
+    first = None
+    for _ in range(3):
+        got = [tcr.selective_scan(v["x"], v["dt"], v["a"], v["b"], v["c"], skip=v["skip"], gate=v["gate"], dt_bias=v["dt_bias"], state=v["state"]),
+               *grads_of(tcr, v, dout, None, None).values()]
+        if first is not None:
+            assert all(torch.equal(p, q) for p, q in zip(first, got))
+        first = got
+
+
+def test_given_outputs_and_strides(tcr):
+    v = make(torch.float16, (2, 45), 40, 16, state=2, seed=9)
+    args, given = (v["x"], v["dt"], v["a"], v["b"], v["c"]), {k: v[k] for k in ("skip", "gate", "dt_bias", "state")}
+    want = tcr.selective_scan(*args, **given)
+    wide = torch.full((2, 45, 44), 7.0, device="cuda", dtype=torch.float16)
+    got = tcr.selective_scan(*args, **given, out=wide[..., 3:43])
+    assert got.data_ptr() == wide[..., 3:].data_ptr() and torch.equal(got, want) and (wide[..., :3] == 7).all() and (wide[..., 43:] == 7).all()
+    # one row for all tokens, other strides
+    turned = {k: v[k].transpose(0, 1).contiguous().transpose(0, 1) if k in ("x", "dt", "gate") else v[k] for k in v}
+    rows = v["x"][:, :1].contiguous().expand(2, 45, 40)
+    assert rows.stride(1) == 0
+    assert torch.equal(tcr.selective_scan(rows, *args[1:], **given), tcr.selective_scan(rows.contiguous(), *args[1:], **given))
+    assert torch.equal(tcr.selective_scan(turned["x"], turned["dt"], *args[2:], **{**given, "gate": turned["gate"]}), want)
+
+
+def test_long_in_chunks_is_the_same_as_in_parts(tcr):
+    """A prompt in two calls, the second going on from the first's states, is the prompt in one: 4000 tokens, whose chunks differ."""
+    v = make(torch.float32, (1, 4000), 70, 16, seed=10)
+    args, given = ("x", "dt", "a", "b", "c"), ("skip", "gate", "dt_bias")
+    whole, last = tcr.selective_scan(*(v[k] for k in args), **{k: v[k] for k in given}, final_state=True)
+    cut = lambda k, s: v[k][:, s] if k not in ("a", "skip", "dt_bias") else v[k]  # noqa: E731
+    first, state = tcr.selective_scan(*(cut(k, slice(0, 1501)) for k in args), **{k: cut(k, slice(0, 1501)) for k in given}, final_state=True)
+    second, end = tcr.selective_scan(*(cut(k, slice(1501, 4000)) for k in args), **{k: cut(k, slice(1501, 4000)) for k in given}, state=state, final_state=True)
+    want, large = (reference(**v, softplus=True, offsets=None, large=m) for m in (False, True))
+    for got in (whole, torch.cat([first, second], 1)):
+        check(got, want[0], large[0], 8 * 4000 + 32, "out")
+        # errors of independent roundings that die out within some hundred tokens
+        assert (got.double() - want[0]).norm() <= 2.0 ** -20 * want[0].norm()
+    for got in (last, end):
+        assert (got.double() - want[1]).norm() <= 2.0 ** -20 * want[1].norm()
+
+
+def test_refusals(tcr):
+    v = make(torch.bfloat16, (2, 8), 16, 16, state=2)
+    args = [v["x"], v["dt"], v["a"], v["b"], v["c"]]
+    bad = [(0, v["x"].cpu()), (0, v["x"].double()), (0, v["x"][0]), (1, v["dt"].float()), (1, v["dt"][:, :4]), (2, v["a"].double()), (2, v["a"].T.contiguous().T),
+           (2, v["a"][:8]), (3, v["b"].float()), (3, v["b"][:, :, 0]), (4, v["c"][..., :8]), (0, v["x"].transpose(0, 2).contiguous().transpose(0, 2))]
+    for i, t in bad:
+        with pytest.raises((TypeError, ValueError)):
+            tcr.selective_scan(*args[:i], t, *args[i + 1:])
+    for more in ({"skip": v["skip"].half()}, {"dt_bias": v["skip"][:8]}, {"gate": v["gate"].float()}, {"state": v["state"].half()}, {"state": v["state"][:1]},
+                 {"out": torch.empty(2, 8, 16, device="cuda")}, {"offsets": torch.tensor([0, 8], device="cuda")}):
+        with pytest.raises((TypeError, ValueError)):
+            tcr.selective_scan(*args, **more)
+    with pytest.raises(ValueError):
+        tcr.selective_scan(*args[:3], v["b"].expand(2, 8, 3, 16).contiguous(), v["c"].expand(2, 8, 3, 16).contiguous())     # 16 channels, 3 groups
+    for i in (0, 1):
+        with pytest.raises(tcr.TcrError):
+            tcr.selective_scan(*args, out=args[i])                                                                          # in an input's place
+    b = torch.randn(2, 8, 1, 65, device="cuda").to(torch.bfloat16)
+    with pytest.raises(tcr.TcrError):
+        tcr.selective_scan(v["x"], v["dt"], torch.zeros(16, 65, device="cuda"), b, b)
+    with pytest.raises(TypeError):
+        tcr.selective_scan_step(*(t[:, 0] if t.dim() > 2 else t for t in args), v["state"][:, :8])
