@@ -1,0 +1,147 @@
+"""Refusals of the convolution, the selective scan and the clipping that need no GPU: they come back as a status before any device work."""
+import ctypes
+
+import pytest
+
+from paper_1811_09736_amd import binding as tcr
+
+BASE = 1 << 20                               # aligned addresses that are never followed
+FAR = 1 << 30
+
+
+def filled(kind, **more):
+    a = kind()
+    for k, v in more.items():
+        if k.endswith("stride"):
+            getattr(a, k)[:] = v
+        else:
+            setattr(a, k, v)
+    return a
+
+
+def conv(**more):
+    return filled(tcr.ConvolutionShape, **{**dict(dtype=tcr.F16, channels=64, width=4, activation=1, sequences=2, tokens=10, offsets=None, x_stride=[640, 64],
+                                                  o_stride=[640, 64]), **more})
+
+
+def scan(**more):
+    wide, narrow = [640, 64], [160, 16, 16]
+    return filled(tcr.SelectiveShape, **{**dict(dtype=tcr.F16, channels=64, states=16, groups=1, softplus=1, sequences=2, tokens=10, offsets=None, a=BASE, skip=None, dt_bias=None,
+                                                x_stride=wide, dt_stride=wide, gate_stride=wide, o_stride=wide, b_stride=narrow, c_stride=narrow), **more})
+
+
+def forward(a, x=BASE, weight=BASE, bias=None, out=FAR, state=None, last=None):
+    return tcr.raw().tcr_causal_conv(None if a is None else ctypes.byref(a), x, weight, bias, out, state, last, None)
+
+
+def selective(a, x=BASE, dt=BASE, b=BASE, c=BASE, gate=None, out=FAR, state=None, last=None):
+    return tcr.raw().tcr_selective_scan(None if a is None else ctypes.byref(a), x, dt, b, c, gate, out, state, last, None)
+
+
+def both(a, name, status):
+    call = forward if isinstance(a, tcr.ConvolutionShape) else selective
+    assert call(a) == status, name
+
+
+@pytest.mark.parametrize("more", [{"dtype": tcr.E4M3}, {"dtype": 9}, {"channels": 0}, {"width": 0}, {"activation": 2}, {"offsets": BASE + 4}], ids=str)
+def test_convolutions_that_are_none(more):
+    assert forward(conv(**more)) == tcr.ERR_INVALID_ARG
+    assert tcr.raw().tcr_causal_conv_backward(ctypes.byref(conv(**more)), *[BASE] * 4, FAR, BASE, None, None, None, None, None) == tcr.ERR_INVALID_ARG
+    assert tcr.raw().tcr_causal_conv_step(ctypes.byref(conv(**{"tokens": 1, **more})), BASE, BASE, None, FAR, BASE, BASE, None) == tcr.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("more", [{"width": 1}, {"width": 5}, {"channels": (1 << 20) + 1}, {"tokens": 1 << 31}, {"sequences": 1 << 40}, {"sequences": 1 << 62, "tokens": 1 << 62}], ids=str)
+def test_convolutions_without_a_kernel(more):
+    assert forward(conv(**more)) == tcr.ERR_UNSUPPORTED
+
+
+def test_convolution_pointers():
+    inv = tcr.ERR_INVALID_ARG
+    assert forward(None) == inv
+    for name in ("x", "weight", "out"):
+        assert forward(conv(), **{name: None}) == inv and forward(conv(), **{name: BASE + 1}) == inv
+    for name in ("bias", "state", "last"):
+        assert forward(conv(), **{name: BASE + 1}) == inv
+    assert forward(conv(), out=BASE) == inv and forward(conv(), out=BASE + 128) == inv                  # x's place
+    assert forward(conv(), state=FAR * 2, last=FAR * 2 + 64) == inv
+    step = tcr.raw().tcr_causal_conv_step
+    assert step(ctypes.byref(conv()), BASE, BASE, None, FAR, BASE, BASE, None) == inv                   # ten tokens
+    assert step(ctypes.byref(conv(tokens=1)), BASE, BASE, None, FAR, None, BASE, None) == inv
+    assert step(ctypes.byref(conv(tokens=1, offsets=BASE)), BASE, BASE, None, FAR, BASE, BASE, None) == inv
+    back = tcr.raw().tcr_causal_conv_backward
+    for i in (0, 1, 2, 4, 5):
+        args = [BASE] * 3 + [None, FAR, BASE, None]
+        args[i] = None
+        assert back(ctypes.byref(conv()), *args, None, None, None, None) == inv
+    assert back(ctypes.byref(conv()), BASE, BASE, BASE, None, BASE, BASE, None, None, None, None, None) == inv          # dx in x's place
+    assert back(ctypes.byref(conv()), BASE, BASE, BASE, None, FAR, BASE, None, FAR * 2, None, FAR * 2, None) == inv     # dstate in state's
+
+
+@pytest.mark.parametrize("more", [{"dtype": tcr.I8}, {"channels": 0}, {"states": 0}, {"groups": 0}, {"groups": 3}, {"softplus": 2}, {"a": None}, {"a": BASE + 2}, {"skip": BASE + 1},
+                                  {"dt_bias": BASE + 2}, {"offsets": BASE + 4}], ids=str)
+def test_scans_that_are_none(more):
+    assert selective(scan(**more)) == tcr.ERR_INVALID_ARG
+    assert tcr.raw().tcr_selective_scan_step(ctypes.byref(scan(**{"tokens": 1, **more})), *[BASE] * 4, None, FAR, BASE, BASE, None) == tcr.ERR_INVALID_ARG
+    assert tcr.raw().tcr_selective_scan_backward(ctypes.byref(scan(**more)), *[BASE] * 5, None, *[BASE] * 5, *[None] * 7) == tcr.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("more", [{"states": 65}, {"channels": 1 << 21}, {"tokens": 1 << 31}, {"sequences": 1 << 40}], ids=str)
+def test_scans_without_a_kernel(more):
+    assert selective(scan(**more)) == tcr.ERR_UNSUPPORTED
+    assert tcr.raw().tcr_selective_scan_backward(ctypes.byref(scan(**more)), *[BASE] * 5, None, *[BASE] * 5, *[None] * 7) == tcr.ERR_UNSUPPORTED
+
+
+def test_scan_pointers():
+    inv = tcr.ERR_INVALID_ARG
+    assert selective(None) == inv
+    for name in ("x", "dt", "b", "c", "out"):
+        assert selective(scan(), **{name: None}) == inv and selective(scan(), **{name: BASE + 1}) == inv
+    assert selective(scan(), gate=BASE + 1) == inv and selective(scan(), state=BASE + 2) == inv and selective(scan(), last=BASE + 1) == inv
+    for name in ("x", "dt", "b", "c", "gate"):
+        assert selective(scan(), **{name: FAR}) == inv                                                  # out in its place
+    assert selective(scan(), state=FAR * 2, last=FAR * 2 + 64) == inv
+    step = tcr.raw().tcr_selective_scan_step
+    assert step(ctypes.byref(scan()), *[BASE] * 4, None, FAR, BASE, BASE, None) == inv
+    assert step(ctypes.byref(scan(tokens=1)), *[BASE] * 4, None, FAR, BASE, None, None) == inv
+    assert step(ctypes.byref(scan(tokens=1, offsets=BASE)), *[BASE] * 4, None, FAR, BASE, BASE, None) == inv
+    back = tcr.raw().tcr_selective_scan_backward
+    good = [BASE] * 5 + [None] + [BASE] * 5 + [None] * 7
+    for i in (0, 1, 2, 3, 4, 6, 7, 8, 9, 10):
+        args = list(good)
+        args[i] = None
+        assert back(ctypes.byref(scan()), *args) == inv
+    for i, p in ((5, BASE), (12, BASE), (11, BASE + 1), (13, BASE + 2), (14, BASE + 1), (15, BASE + 1), (16, BASE + 2)):      # a gate without dgate, dgate without a gate, alignment
+        args = list(good)
+        args[i] = p
+        assert back(ctypes.byref(scan()), *args) == inv
+    args = list(good)
+    args[14] = args[16] = FAR
+    assert back(ctypes.byref(scan()), *args) == inv                                                     # dstate in state's place
+
+
+def test_clipping():
+    inv = tcr.ERR_INVALID_ARG
+    call, norm = tcr.raw().tcr_clip_gradients, tcr.raw().tcr_gradient_norm
+
+    def places(*entries):
+        return (tcr.TensorPlace * max(1, len(entries)))(*(tcr.TensorPlace(*e) for e in entries))
+
+    def to(*at):
+        return (ctypes.c_void_p * len(at))(*at)
+
+    one = places((BASE, 100, tcr.F32))
+    assert norm(one, 1, None, None) == inv and norm(one, 1, FAR + 2, None) == inv and norm(None, 1, FAR, None) == inv
+    assert norm(places((None, 100, tcr.F32)), 1, FAR, None) == inv and norm(places((BASE + 2, 100, tcr.F32)), 1, FAR, None) == inv
+    assert norm(places((BASE, 100, tcr.E4M3)), 1, FAR, None) == inv
+    assert norm(places((BASE, (1 << 40) + 1, tcr.F16)), 1, FAR, None) == tcr.ERR_UNSUPPORTED
+    assert norm(places((BASE, 1 << 40, tcr.F16), (BASE, 1, tcr.F16)), 2, FAR, None) == tcr.ERR_UNSUPPORTED
+    for limit, eps in ((-1.0, 0.0), (float("nan"), 0.0), (1.0, -1.0), (1.0, float("nan"))):
+        assert call(one, None, 1, limit, eps, FAR, None) == inv
+    two = places((BASE, 100, tcr.F32), (BASE + 396, 100, tcr.F32))
+    assert call(two, None, 2, 1.0, 0.0, FAR, None) == inv                                               # the second begins in the first
+    assert call(one, None, 1, 1.0, 0.0, BASE + 8, None) == inv                                          # the norm in a tensor
+    apart = places((BASE, 100, tcr.F32), (BASE + 400, 100, tcr.F32))
+    assert call(apart, to(FAR, FAR + 396), 2, 1.0, 0.0, FAR * 2, None) == inv
+    assert call(apart, to(BASE + 400, BASE), 2, 1.0, 0.0, FAR * 2, None) == inv                         # in each other's place
+    assert call(apart, to(BASE + 4, FAR), 2, 1.0, 0.0, FAR * 2, None) == inv
+    assert call(apart, to(FAR, None), 2, 1.0, 0.0, FAR * 2, None) == inv
