@@ -1,5 +1,5 @@
-"""Linear attention with decay and the root-mean-square norm as differentiable functions: binding's calls and their gradients, nothing else
-(gradients of the gradients are refused)."""
+"""Linear attention with decay, the root-mean-square norm, the short causal convolution and the selective scan as differentiable functions: binding's calls
+and their gradients, nothing else (gradients of the gradients are refused)."""
 from __future__ import annotations
 
 import torch
@@ -63,3 +63,55 @@ class _RmsNorm(torch.autograd.Function):
 def rms_norm(x, weight, residual=None, eps=1e-6):
     """binding.rms_norm with gradients for x, weight and residual: the norm, with a residual (the norm, x + residual)."""
     return _RmsNorm.apply(x, weight, residual, eps)
+
+
+def _whole(grad, like):
+    """The gradient of an output of `like`'s shape: zeros where the output was not used, its last dimension contiguous."""
+    if grad is None:
+        return torch.zeros(like.shape, dtype=like.dtype, device=like.device)
+    return grad if grad.stride(-1) == 1 else grad.contiguous()
+
+
+class _CausalConv(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, activation, offsets, state):
+        ctx.save_for_backward(x, weight, bias, offsets, state)
+        ctx.activation = activation
+        ctx.set_materialize_grads(False)
+        return binding.causal_conv(x, weight, bias=bias, activation=activation, offsets=offsets, state=state, final_state=True)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout, dlast):
+        x, weight, bias, offsets, state = ctx.saved_tensors
+        dx, dweight, dbias, dstate = binding.causal_conv_backward(_whole(dout, x), x, weight, bias=bias, activation=ctx.activation, offsets=offsets, state=state,
+                                                                  dfinal=None if dlast is None else dlast.contiguous())
+        return dx, dweight, dbias, None, None, dstate
+
+
+def causal_conv(x, weight, bias=None, activation="silu", offsets=None, state=None):
+    """binding.causal_conv with gradients for x, weight, bias and state: (out, the last width - 1 inputs of every sequence)."""
+    return _CausalConv.apply(x, weight, bias, activation, offsets, state)
+
+
+class _SelectiveScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, state):
+        ctx.save_for_backward(x, dt, a, b, c, skip, gate, dt_bias, offsets, state)
+        ctx.softplus = softplus
+        ctx.set_materialize_grads(False)
+        return binding.selective_scan(x, dt, a, b, c, skip=skip, gate=gate, dt_bias=dt_bias, softplus=softplus, offsets=offsets, state=state, final_state=True)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout, dlast):
+        x, dt, a, b, c, skip, gate, dt_bias, offsets, state = ctx.saved_tensors
+        dx, ddt, da, db, dc, dskip, dgate, dbias, dstate = binding.selective_scan_backward(
+            _whole(dout, x), x, dt, a, b, c, skip=skip, gate=gate, dt_bias=dt_bias, softplus=ctx.softplus, offsets=offsets, state=state,
+            dfinal=None if dlast is None else dlast.contiguous())
+        return dx, ddt, da, db, dc, dskip, dgate, dbias, None, None, dstate
+
+
+def selective_scan(x, dt, a, b, c, skip=None, gate=None, dt_bias=None, softplus=True, offsets=None, state=None):
+    """binding.selective_scan with gradients for x, dt, a, b, c, skip, gate, dt_bias and state: (out, the states behind the last tokens)."""
+    return _SelectiveScan.apply(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, state)

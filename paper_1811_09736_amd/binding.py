@@ -183,6 +183,9 @@ def _load_native():
     _native.bind_layers(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
         "tcr_linear_attention", "tcr_linear_attention_step", "tcr_linear_attention_backward", "tcr_rms_norm", "tcr_rms_norm_quantized",
         "tcr_rms_norm_backward")))
+    _native.bind_selective(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
+        "tcr_causal_conv", "tcr_causal_conv_step", "tcr_causal_conv_backward", "tcr_selective_scan", "tcr_selective_scan_step",
+        "tcr_selective_scan_backward", "tcr_gradient_norm", "tcr_clip_gradients")))
     return _native
 
 
@@ -744,6 +747,10 @@ def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tens
     x [B, T, D], or packed sequences [M, D] with `offsets` ([sequences + 1], int64); weight [D, width], bias [D] (2 <= width <= 4); activation "silu" or
     None.  state [sequences, width - 1, D]: the inputs in front of the first tokens, the oldest first.  All of x's type.  Returns out like x (a given one
     not x), with final_state also the last width - 1 inputs of every sequence."""
+    if stream is None:
+        got = _native.causal_conv(x, weight, bias, activation, offsets, out, state, final_state)
+        if got is not None:
+            return got
     given = out
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -760,6 +767,10 @@ def causal_conv_step(x: torch.Tensor, weight: torch.Tensor, state: torch.Tensor,
                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """tcr_causal_conv_step: one token for every sequence.  x [B, D], state [B, width - 1, D].  The new states go to new_state, without it to `state`
     itself.  Returns out [B, D]."""
+    if stream is None:
+        got = _native.causal_conv_step(x, weight, bias, activation, None, out, state, new_state)
+        if got is not None:
+            return got
     given = out
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -779,6 +790,10 @@ def causal_conv_backward(dout: torch.Tensor, x: torch.Tensor, weight: torch.Tens
                          dfinal: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """tcr_causal_conv_backward: (dx, dweight, dbias, dstate) from dout and, where the final states were used, their gradient dfinal.  dbias is None
     without a bias, dstate without `state`."""
+    if stream is None:
+        got = _native.causal_conv_backward(x, weight, bias, activation, offsets, dout, state, dfinal)
+        if got is not None:
+            return got
     shape, states = _convolution(x, weight, bias, activation, offsets, dout)
     _whole_of(state, "state", states, x)
     _whole_of(dfinal, "dfinal", states, x)
@@ -816,6 +831,10 @@ def selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.
     x, dt, gate [B, T, D], b, c [B, T, G, N], D a multiple of G; or packed sequences [M, D], [M, G, N] with `offsets` ([sequences + 1], int64).  a [D, N],
     skip, dt_bias [D], float32.  softplus=False: d_t = dt_t + dt_bias.  state [sequences, D, N], float32: the states to go on from.
     Returns out [B, T, D] ([M, D]; a given one none of the inputs), with final_state also the states behind the last tokens."""
+    if stream is None:
+        got = _native.selective_scan(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, out, state, final_state)
+        if got is not None:
+            return got
     given = out
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -835,6 +854,10 @@ def selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: t
                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """tcr_selective_scan_step: one token for every sequence.  x, dt, gate [B, D], b, c [B, G, N], state [B, D, N].  The new states go to new_state,
     without it to `state` itself.  Returns out [B, D]."""
+    if stream is None:
+        got = _native.selective_scan_step(x, dt, a, b, c, skip, gate, dt_bias, softplus, None, out, state, new_state)
+        if got is not None:
+            return got
     given = out
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -856,6 +879,10 @@ def selective_scan_backward(dout: torch.Tensor, x: torch.Tensor, dt: torch.Tenso
                             dfinal: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """tcr_selective_scan_backward: (dx, ddt, da, db, dc, dskip, dgate, ddt_bias, dstate) from dout and, where the final states were used, their gradient
     dfinal.  None in the place of what was not given: skip, gate, dt_bias, state."""
+    if stream is None:
+        got = _native.selective_scan_backward(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, dout, state, dfinal)
+        if got is not None:
+            return got
     shape = _selective(x, dt, a, b, c, skip, gate, dt_bias, softplus, offsets, dout)
     states = (shape.sequences, shape.channels, shape.states)
     _constants_of(state, "state", states, x)
@@ -900,6 +927,10 @@ def _norm_of(tensors) -> torch.Tensor:
 
 def gradient_norm(tensors, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """tcr_gradient_norm: the Euclidean norm of all the tensors' elements together, a float32 tensor without dimensions."""
+    if stream is None:
+        got = _native.gradient_norm(tensors)
+        if got is not None:
+            return got
     tensors, places = _places(tensors)
     norm = _norm_of(tensors)
     _run(_lib.tcr_gradient_norm, "tcr_gradient_norm", norm, stream, places, len(tensors), norm.data_ptr())
@@ -909,6 +940,10 @@ def gradient_norm(tensors, stream: Optional[torch.cuda.Stream] = None) -> torch.
 def clip_gradients(tensors, max_norm: float, eps: float = 1e-6, out=None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """tcr_clip_gradients: scales the tensors by min(1, max_norm / (norm + eps)), in place, or to the tensors `out` of the same types, shapes and strides.
     Returns their norm in front of it, a float32 tensor without dimensions.  No tensor may stand twice in the list."""
+    if stream is None:
+        got = _native.clip_gradients(tensors, max_norm, eps, out)
+        if got is not None:
+            return got
     tensors, places = _places(tensors)
     to = None
     if out is not None:

@@ -18,6 +18,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
+#include <vector>
 
 #include "../../include/tcr.h"
 
@@ -267,12 +268,15 @@ PyObject* bind(PyObject*, PyObject* args) {
 }
 
 #include "layers/tcr_native_layers.hpp"
+#include "layers/tcr_native_selective.hpp"
 
 #define TCR_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {TCR_FAST(segmented_reduce), TCR_FAST(segmented_scan), TCR_FAST(scan), TCR_FAST(reduce), TCR_FAST(segmented_moments),
                            TCR_FAST(irregular_reduce), TCR_FAST(irregular_moments), TCR_FAST(irregular_scan),
                            TCR_FAST(linear_attention), TCR_FAST(linear_attention_step), TCR_FAST(linear_attention_backward), TCR_FAST(rms_norm),
                            TCR_FAST(rms_norm_quantized), TCR_FAST(rms_norm_backward), {"bind_layers", bind_layers, METH_VARARGS, nullptr},
+                           TCR_FAST(causal_conv), TCR_FAST(causal_conv_step), TCR_FAST(causal_conv_backward), TCR_FAST(selective_scan), TCR_FAST(selective_scan_step),
+                           TCR_FAST(selective_scan_backward), TCR_FAST(gradient_norm), TCR_FAST(clip_gradients), {"bind_selective", bind_selective, METH_VARARGS, nullptr},
                            {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "The ordinary calls of binding.py (see there).", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
