@@ -8,12 +8,13 @@ using tcr::host::partials_for;
 
 namespace {
 
-// Wavefronts that a scan is cut for, and chunks of a sequence at most: each looks through the ones in front of it.
-constexpr uint64_t kFillWaves = 2048, kMostChunks = 64;
+// Wavefronts that a scan is cut for -- four on each SIMD: 8192 tokens x 4096 channels x 16 states 272 us, with two 325, with eight 274 -- and chunks of a sequence at
+// most: each looks through the ones in front of it.
+constexpr uint64_t kFillWaves = 4096, kMostChunks = 64;
 
 template <typename T, int K, int P>
 tcr_status run(Selective s, hipStream_t stream) {
-    constexpr uint32_t kTile = 8 * P, kStates = K * P, kChannels = Slab<P>::kChannels;
+    constexpr uint32_t kStates = K * P, kChannels = Slab<P>::kChannels, kTile = 8 * P;
     const uint64_t spans = s.offsets != nullptr ? 1 : s.sequences;
     if (spans == 0) return TCR_OK;
     s.slabs = (uint32_t)div_up(s.channels / s.groups, kChannels);

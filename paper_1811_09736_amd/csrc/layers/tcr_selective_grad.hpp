@@ -18,8 +18,6 @@
 namespace tcr {
 namespace layers {
 
-constexpr int kTurn = 8;
-
 struct SelectiveGrad {
     Selective s;                               // out: dout
     const float* dfinal;                       // NULL: none

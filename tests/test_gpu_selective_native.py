@@ -10,11 +10,17 @@ def flat(r):
     return [t for t in (r if isinstance(r, tuple) else (r,)) if t is not None]
 
 
+def bits(x):
+    return x.contiguous().reshape(-1).view(torch.int32 if x.element_size() == 4 else torch.int16)
+
+
 def same(a, b):
+    """Bit for bit: random steps without a softplus are negative too, and a state that grows by exp(2.5) a token leaves the range within 37 tokens: NaN on both sides."""
     a, b = flat(a), flat(b)
     assert len(a) == len(b)
     for x, y in zip(a, b):
-        assert x.dtype == y.dtype and x.shape == y.shape and x.device == y.device and not x.requires_grad and torch.equal(x, y)
+        assert x.dtype == y.dtype and x.shape == y.shape and x.device == y.device and not x.requires_grad
+        assert torch.equal(bits(x), bits(y))
 
 
 def test_what_is_no_gpu_tensor_is_left_to_binding():
