@@ -364,8 +364,9 @@ tcr_status tcr_selective_scan_step(const tcr_selective *shape, const void *x, co
  * Gradients of tcr_selective_scan.  dout is laid out by o_stride; dx, ddt, dgate (NULL where gate is) are contiguous (sequence, token, channel -- packed: token, channel),
  * db and dc (sequence, token, group, state), summed over a group's channels; da, dskip, ddt_bias (NULL: not wanted) like a, skip and dt_bias, summed over all tokens: the
  * same from run to run.  None of them stands in an input's place (not checked but for dstate).  state: the forward call's; dfinal: the gradient of its final_state (NULL: none);
- * dstate: the gradient of `state` (NULL: not wanted).  With p the power of two from 4 to 64 that holds the states, workspace of about tokens * channels * (4 + p * p / 128) bytes
- * -- 6 for 16 states -- and 12 * channels for each sequence; with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, and nothing done.
+ * dstate: the gradient of `state` (NULL: not wanted).  Takes up to 6, 6, 7, 17 or 49 bytes of workspace for each token and channel with up to 4, 8, 16, 32 or 64 states, the
+ * channels of each group rounded up to a multiple of 256, 128, 64, 32 or 16, and as much as for 32 tokens more for each sequence; of a caller's buffer that is the second half of what
+ * follows its first 256 bytes.  With less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, and nothing done.
  */
 tcr_status tcr_selective_scan_backward(const tcr_selective *shape, const void *dout, const void *x, const void *dt, const void *b, const void *c,
                                        const void *gate, void *dx, void *ddt, float *da, void *db, void *dc, float *dskip, void *dgate, float *ddt_bias,

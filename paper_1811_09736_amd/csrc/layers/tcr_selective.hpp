@@ -83,7 +83,7 @@ __device__ __forceinline__ float swap_add16(float a, float b) {
 }
 template <int CTRL>
 __device__ __forceinline__ float dpp_of(float x) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false));
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
 constexpr int kRor4 = 0x124, kRor8 = 0x128;
 template <int P>

@@ -36,7 +36,7 @@ tcr_status run(SelectiveGrad g, hipStream_t stream) {
         if (s.per_span > 1) {
             selective_parts_kernel<T, P><<<grid_of(blocks), kScanThreads, 0, stream>>>(g, (uint32_t)blocks);
             if (launched("selective_parts_kernel") != TCR_OK) return TCR_ERR_HIP;
-            selective_carry_kernel<kStates><<<dim3((unsigned)div_up(spans * all * kStates, kScanThreads), 2), kScanThreads, 0, stream>>>(g, all);
+            selective_carry_kernel<kStates><<<dim3((unsigned)div_up(spans * all * kStates, 64), 2), 64 * kCarryLines, 0, stream>>>(g, all);
             if (launched("selective_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
         }
         selective_grad_kernel<T, P><<<grid_of(blocks), kScanThreads, 0, stream>>>(g, (uint32_t)blocks);

@@ -29,7 +29,8 @@ struct SelectiveGrad {
     uint32_t* closed;                          // [chunk] whether a bound lies in it, so that nothing passes through; NULL: none do
 };
 
-template <int P> constexpr int kGradTile = P == 16 ? 64 : 8 * P;
+// Tokens of a chunk: a vector for each thread, but no more than leave room for two workgroups and more in LDS (32 states, 2048 tokens x 2048 channels: 64 tokens 356 us, 32 240).
+template <int P> constexpr int kGradTile = P >= 8 ? 32 : 8 * P;
 
 // The inputs of a tile, as each thread has loaded eight channels of a token, and as they stand in LDS.
 template <typename T, int P>
@@ -37,12 +38,11 @@ struct GradTile {
     static constexpr int kTile = kGradTile<P>, kChannels = Slab<P>::kChannels, kStates = 4 * P, kRow = kChannels / kVec;
     typedef typename Vec<T>::v vec;
     uint32_t token, wide, first;               // this thread's
-    bool there;
+    bool there, inside;                        // inside: of a sequence
     vec x, gate, dout;
     float raw[kVec], d[kVec], dy[kVec];
 
-    __device__ __forceinline__ void load(const SelectiveGrad& g, const Slab<P>& slab, uint32_t t0, uint32_t t1, uint32_t begin, uint32_t finish,
-                                         float (*du)[kChannels][2], float (*dys)[kChannels], float (*bs)[kStates], float (*cs)[kStates]) {
+    __device__ __forceinline__ void load(const SelectiveGrad& g, const Slab<P>& slab, uint32_t t0, uint32_t t1, uint32_t begin, uint32_t finish) {
         const Selective& s = g.s;
         const uint32_t tid = threadIdx.x;
         token = tid / kRow;
@@ -50,7 +50,6 @@ struct GradTile {
         first = slab.first + wide;
         const uint32_t t = t0 + token;
         there = token < kTile && t < t1 && first < slab.end;
-        const bool inside = there && t >= begin && t < finish;
         x = dout = gate = vec{};
         vec dt = {};
         if (there) {
@@ -59,22 +58,40 @@ struct GradTile {
             dout = load_raw(static_cast<const T*>(s.out) + slab.span * s.out_seq + t * s.out_tok, first, slab.end);
             if (s.gate.p != nullptr) gate = load_raw(static_cast<const T*>(s.gate.p) + slab.span * s.gate.seq + t * s.gate.tok, first, slab.end);
         }
-        if (token < kTile)
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                raw[i] = (float)dt[i] + (s.bias != nullptr && first + i < slab.end ? s.bias[first + i] : 0.0f);
-                // (outside of all sequences: nothing)
-                d[i] = inside ? s.softplus ? softplus_of(raw[i]) : raw[i] : 0.0f;
-                float v = (float)dout[i];
-                if (s.gate.p != nullptr) v *= (float)gate[i] * sigmoid_of((float)gate[i]);
-                dy[i] = inside ? v : 0.0f;
-                du[token][wide + i][0] = d[i];
-                du[token][wide + i][1] = inside ? d[i] * (float)x[i] : 0.0f;
-                dys[token][wide + i] = dy[i];
-            }
+        for (int i = 0; i < kVec; ++i) raw[i] = 0.0f;
+        if (s.bias != nullptr && there) load_vec(s.bias, (uint64_t)first, (uint64_t)slab.end, raw);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            raw[i] += (float)dt[i];
+            d[i] = raw[i];
+            dy[i] = (float)dout[i];
+        }
+        if (s.softplus)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) d[i] = softplus_of(raw[i]);
+        if (s.gate.p != nullptr)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) dy[i] *= (float)gate[i] * sigmoid_of((float)gate[i]);
+        inside = there && t >= begin && t < finish;
+    }
+    __device__ __forceinline__ void put(const SelectiveGrad& g, const Slab<P>& slab, uint32_t t0, uint32_t t1, uint32_t begin, uint32_t finish, float (*ds)[kChannels],
+                                        float (*us)[kChannels], float (*dys)[kChannels], float (*bs)[kStates], float (*cs)[kStates]) {
+        const Selective& s = g.s;
+        float u[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) u[i] = d[i] * (float)x[i];
+        if (!inside)                           // outside of all sequences: nothing
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) d[i] = u[i] = dy[i] = 0.0f;
+        if (token < kTile) {
+            put_vec(ds[token] + wide, d);
+            put_vec(us[token] + wide, u);
+            put_vec(dys[token] + wide, dy);
+        }
         const T* const b = static_cast<const T*>(s.b.p) + slab.span * s.b.seq + slab.group * s.b.group;
         const T* const c = static_cast<const T*>(s.c.p) + slab.span * s.c.seq + slab.group * s.c.group;
-        for (uint32_t e = tid; e < kTile * kStates; e += kScanThreads) {
+        for (uint32_t e = threadIdx.x; e < kTile * kStates; e += kScanThreads) {
             const uint32_t bt = t0 + e / kStates, n = e % kStates;
             const bool any = bt < t1 && bt >= begin && bt < finish && n < s.states;
             bs[e / kStates][n] = any ? (float)b[bt * s.b.tok + n] : 0.0f;
@@ -88,7 +105,7 @@ template <typename T, int P>
 __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(SelectiveGrad g, uint32_t blocks) {
     typedef GradTile<T, P> Tile;
     constexpr int K = 4, kWide = 64 / P, kTile = Tile::kTile, kStates = Tile::kStates, kChannels = Tile::kChannels;
-    __shared__ float du[kTile][kChannels][2], dys[kTile][kChannels], bs[kTile][kStates], cs[kTile][kStates];
+    __shared__ __attribute__((aligned(16))) float ds[kTile][kChannels], us[kTile][kChannels], dys[kTile][kChannels], bs[kTile][kStates], cs[kTile][kStates];
     if (workgroup() >= blocks) return;
     const Selective& s = g.s;
     const Slab<P> slab(s, s.per_span);
@@ -99,8 +116,11 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
     const uint32_t begin = s.offsets != nullptr ? bounds.at(0) : 0, finish = s.offsets != nullptr ? bounds.at(bounds.count) : s.span;
     Place at;
     at.find(bounds, slab.span, t0);
-    Tile tile;
-    tile.load(g, slab, t0, t1, begin, finish, du, dys, bs, cs);
+    {
+        Tile tile;
+        tile.load(g, slab, t0, t1, begin, finish);
+        tile.put(g, slab, t0, t1, begin, finish, ds, us, dys, bs, cs);
+    }
     float rate[K], h[K], pass[K], back[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -116,7 +136,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
     __syncthreads();
     float sum = 0.0f;
     auto token = [&](uint32_t j) {
-        const float d = du[j][wide][0], u = du[j][wide][1], dy = dys[j][wide];
+        const float d = ds[j][wide], u = us[j][wide], dy = dys[j][wide];
         sum += d;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -166,17 +186,21 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
     if (g.closed != nullptr && threadIdx.x == 0) g.closed[id] = !open;
 }
 
-// From chunks' own results to what reaches them: s.ends[i] becomes the state in front of chunk i, g.back[i] the gradient behind it.  A thread for each padded channel and state;
-// forwards in the first row of workgroups, backwards in the second.
+// From chunks' own results to what reaches them: s.ends[i] becomes the state in front of chunk i, g.back[i] the gradient behind it.  A column of threads for each padded
+// channel and state, eight chunks a thread, a round of chunks for all of them: each thread makes one step of its eight, takes what the threads in front of it and the rounds before
+// bring, and goes over its eight again.  Forwards in the first row of workgroups, backwards in the second.  (64 chunks of 131072 columns 24 us, as many bytes as it has to move;
+// 96 chunks of 8192 columns, one thread a column from chunk to chunk: 37 us.)
+constexpr int kCarryLines = 8, kCarryChunks = 8;
 template <int NP>
-__global__ __launch_bounds__(kScanThreads) void selective_carry_kernel(SelectiveGrad g, uint64_t all) {
+__global__ __launch_bounds__(64 * kCarryLines) void selective_carry_kernel(SelectiveGrad g, uint64_t all) {
+    __shared__ float steps[2][kCarryLines][64], sums[2][kCarryLines][64];
+    __shared__ bool closed[2][kCarryLines][64];
     const Selective& s = g.s;
-    constexpr int kAhead = 8;
-    constexpr float kNothing = -1.0f;          // no factor is negative
     const uint64_t spans = s.offsets != nullptr ? 1 : s.sequences, one = all * NP;
-    const uint64_t at = (uint64_t)blockIdx.x * kScanThreads + threadIdx.x;
-    if (at >= spans * one) return;
-    const uint64_t span = at / one, rest = at % one, padded = rest / NP;
+    const uint32_t lane = threadIdx.x % 64, line = threadIdx.x / 64;
+    const uint64_t at = (uint64_t)blockIdx.x * 64 + lane;
+    const bool real = at < spans * one;
+    const uint64_t span = real ? at / one : 0, rest = real ? at % one : 0, padded = rest / NP;
     const uint32_t n = rest % NP;
     // (the channel that stands there)
     const uint64_t each = s.channels / s.groups, group_wide = all / s.groups, in_group = padded % group_wide, ch = padded / group_wide * each + in_group;
@@ -184,22 +208,47 @@ __global__ __launch_bounds__(kScanThreads) void selective_carry_kernel(Selective
     const bool backwards = blockIdx.y != 0;
     float* const values = backwards ? g.back : s.ends;
     float carry = 0.0f;
-    for (uint32_t first = 0; first < s.per_span; first += kAhead) {
-        float v[kAhead], keep[kAhead];
+    uint32_t turn = 0;
+    for (uint32_t base = 0; base < s.per_span; base += kCarryLines * kCarryChunks, turn ^= 1) {
+        float v[kCarryChunks], keep[kCarryChunks];
+        bool open[kCarryChunks];
+        const uint32_t first = base + line * kCarryChunks;
+        // (all loads first, the last chunk's again where there are fewer)
+        auto id_of = [&](int i) {
+            const uint32_t c = first + i < s.per_span ? first + i : s.per_span - 1;
+            return (backwards ? s.per_span - 1 - c : c) * spans + span;
+        };
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (first + i >= s.per_span) break;
-            const uint32_t c = backwards ? s.per_span - 1 - first - i : first + i;
-            const uint64_t id = c * spans + span;
+        for (int i = 0; i < kCarryChunks; ++i) {
+            const uint64_t id = id_of(i);
             v[i] = values[id * one + rest];
-            keep[i] = g.closed != nullptr && g.closed[id] ? kNothing : __builtin_amdgcn_exp2f(rate * s.sums[id * all + padded]);
+            keep[i] = s.sums[id * all + padded];
+            open[i] = g.closed == nullptr || g.closed[id] == 0;
+        }
+        float step = 1.0f, sum = 0.0f;
+        bool shut = false;
+#pragma unroll
+        for (int i = 0; i < kCarryChunks; ++i) {
+            keep[i] = __builtin_amdgcn_exp2f(rate * keep[i]);
+            if (first + i >= s.per_span) break;
+            sum = open[i] ? __builtin_fmaf(keep[i], sum, v[i]) : v[i];
+            step *= keep[i];
+            shut |= !open[i];
+        }
+        steps[turn][line][lane] = step;
+        sums[turn][line][lane] = sum;
+        closed[turn][line][lane] = shut;
+        __syncthreads();
+        float mine = carry;
+        for (uint32_t l = 0; l < kCarryLines; ++l) {
+            if (l == line) mine = carry;
+            carry = closed[turn][l][lane] ? sums[turn][l][lane] : __builtin_fmaf(steps[turn][l][lane], carry, sums[turn][l][lane]);
         }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < kCarryChunks; ++i) {
             if (first + i >= s.per_span) break;
-            const uint32_t c = backwards ? s.per_span - 1 - first - i : first + i;
-            values[(c * spans + span) * one + rest] = carry;
-            carry = keep[i] == kNothing ? v[i] : __builtin_fmaf(keep[i], carry, v[i]);
+            if (real) values[id_of(i) * one + rest] = mine;
+            mine = open[i] ? __builtin_fmaf(keep[i], mine, v[i]) : v[i];
         }
     }
 }
@@ -207,7 +256,10 @@ __global__ __launch_bounds__(kScanThreads) void selective_carry_kernel(Selective
 // Sums over the 64 / P channels of a wavefront that stand side by side in the low bits of the lane, of eight values at once; each step leaves half as many to each lane.
 // Lane l ends with the sum of value share_value<P>(l, i) in v[i], i < share_count<P>.
 template <int CTRL>
-__device__ __forceinline__ float add_dpp(float x) { return x + dpp_of<CTRL>(x); }
+__device__ __forceinline__ float add_dpp(float x) {
+#pragma clang fp contract(off)
+    return x + dpp_of<CTRL>(x);                // (contracted with the product that x is, the lanes' exchange would be an operation of its own)
+}
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141;
 template <int P> constexpr int share_count = P == 16 ? 2 : 1;
 template <int P>
@@ -218,11 +270,6 @@ __device__ __forceinline__ int share_value(int lane, int i) {
     if (P == 4) return 4 * b3 + 2 * b2 + b1;
     if (P == 8) return 4 * b2 + 2 * b1 + b0;
     return 4 * b1 + 2 * b0 + i;
-}
-// Whether the lane is the one of those with the same sum that writes it.
-template <int P>
-__device__ __forceinline__ bool share_writer(int lane) {
-    return P == 1 ? (lane & 7) == 0 : P == 2 ? (lane & 3) == 0 : P == 4 ? (lane & 1) == 0 : true;
 }
 template <int CTRL, int COUNT>
 __device__ __forceinline__ void halve(float* v, bool high) {
@@ -263,12 +310,12 @@ __device__ __forceinline__ void sum_shares(float (&v)[8], int lane) {
 }
 
 template <typename T, int P>
-__global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveGrad g, uint32_t blocks) {
+__global__ __launch_bounds__(kScanThreads, 3) void selective_grad_kernel(SelectiveGrad g, uint32_t blocks) {
     typedef GradTile<T, P> Tile;
     constexpr int K = 4, kWide = 64 / P, kTile = Tile::kTile, kStates = Tile::kStates, kChannels = Tile::kChannels, kTurns = kTile / kTurn;
-    __shared__ float du[kTile][kChannels][2];              // d, d x; then sum g b and sum g a exp(d a) h
-    __shared__ float dys[kTile][kChannels];                // dy; then y
-    __shared__ float bs[kTile][kStates], cs[kTile][kStates];
+    __shared__ __attribute__((aligned(16))) float ds[kTile][kChannels], us[kTile][kChannels];          // d, d x; then sum g b and sum g a exp(d a) h
+    __shared__ __attribute__((aligned(16))) float dys[kTile][kChannels];                               // dy; then y
+    __shared__ __attribute__((aligned(16))) float bs[kTile][kStates], cs[kTile][kStates];
     __shared__ float fronts[kTurns][K][kScanThreads];      // the states in front of each turn
     __shared__ float shares[2][4][kTurn][2 * kStates];     // a turn's sums of db and dc over each wavefront's channels
     if (workgroup() >= blocks) return;
@@ -281,8 +328,11 @@ __global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveG
     const uint32_t begin = s.offsets != nullptr ? bounds.at(0) : 0, finish = s.offsets != nullptr ? bounds.at(bounds.count) : s.span;
     const uint64_t spans = s.offsets != nullptr ? 1 : s.sequences, all = (uint64_t)s.slabs * s.groups * kChannels, id = slab.chunk * spans + slab.span;
     const uint64_t place = id * all + slab.padded + wide;
-    Tile tile;
-    tile.load(g, slab, t0, t1, begin, finish, du, dys, bs, cs);
+    {
+        Tile tile;
+        tile.load(g, slab, t0, t1, begin, finish);
+        tile.put(g, slab, t0, t1, begin, finish, ds, us, dys, bs, cs);
+    }
     float rate[K], h[K], back[K], da[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -316,7 +366,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveG
         if ((at.start < t || !starts) && (at.next > t + kTurn || !stops)) quiet |= 1u << turn;
         if (turn + 1 == kTurns || t + kTurn >= t1) break;
         auto token = [&](uint32_t i) {
-            const float d = du[i][wide][0], u = du[i][wide][1];
+            const float d = ds[i][wide], u = us[i][wide];
 #pragma unroll
             for (int k = 0; k < K; ++k) h[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * rate[k]), h[k], u * bs[i][n0 + k]);
         };
@@ -348,7 +398,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveG
                 ahead.pass(bounds, t + i);
                 load_states(ahead.inside ? s.state : nullptr, ahead.seq, s, ch, n0, real, h);
             }
-            const float d = du[j + i][wide][0], u = du[j + i][wide][1];
+            const float d = ds[j + i][wide], u = us[j + i][wide];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 a[i][k] = __builtin_amdgcn_exp2f(d * rate[k]);
@@ -363,7 +413,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveG
             for (int m = kTokens - 1; m >= 0; --m) {
                 const int i = half * kTokens + m;
                 if (!kPlain && at.inside && at.next == t + i + 1) load_states(g.dfinal, at.seq, s, ch, n0, real, back);
-                const float d = du[j + i][wide][0], u = du[j + i][wide][1], dy = dys[j + i][wide];
+                const float d = ds[j + i][wide], u = us[j + i][wide], dy = dys[j + i][wide];
                 float y = 0.0f, gb = 0.0f, w = 0.0f, v[8];
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
@@ -387,12 +437,12 @@ __global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveG
                 gbs[m] = gb;
                 ws[m] = w;
                 sum_shares<P>(v, lane);
-                if (share_writer<P>(lane))
+                // (lanes with the same sum all write it: a branch here would part the tokens' operations)
 #pragma unroll
-                    for (int e = 0; e < share_count<P>; ++e) {
-                        const int value = share_value<P>(lane, e);
-                        shares[turn & 1][wave][i][(value >> 2) * kStates + n0 + (value & 3)] = v[e];
-                    }
+                for (int e = 0; e < share_count<P>; ++e) {
+                    const int value = share_value<P>(lane, e);
+                    shares[turn & 1][wave][i][(value >> 2) * kStates + n0 + (value & 3)] = v[e];
+                }
             }
             sum_parts<P>(ys);
             sum_parts<P>(gbs);
@@ -400,8 +450,8 @@ __global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveG
 #pragma unroll
             for (int i = 0; i < sum_count<P>; ++i) {
                 const uint32_t to = j + half * kTokens + sum_token<P>(lane, i);
-                du[to][wide][0] = gbs[i];
-                du[to][wide][1] = ws[i];
+                ds[to][wide] = gbs[i];
+                us[to][wide] = ws[i];
                 dys[to][wide] = ys[i];
             }
         }
@@ -431,45 +481,61 @@ __global__ __launch_bounds__(kScanThreads) void selective_grad_kernel(SelectiveG
                 store_states(g.dstate, e, s, ch, n0, real, h);
             }
 
-    // what is each token's and channel's own, by the threads that loaded it
-    float to_skip[kVec], to_bias[kVec];
+    // What is each token's and channel's own, by the threads that loaded it: loaded once more, as the registers are the turns' (two wavefronts on a SIMD with them
+    // kept, three without).
+    Tile tile;
+    tile.load(g, slab, t0, t1, begin, finish);
+    const uint32_t t = t0 + tile.token;
+    const bool inside = tile.inside;
     if (tile.token < kTile) {
-        float dx[kVec], ddt[kVec], dz[kVec];
-        const uint32_t t = t0 + tile.token;
+        float gb[kVec], w[kVec], y[kVec], skip[kVec], dx[kVec], ddt[kVec];
+        get_vec(ds[tile.token] + tile.wide, gb);
+        get_vec(us[tile.token] + tile.wide, w);
+        get_vec(dys[tile.token] + tile.wide, y);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) skip[i] = 0.0f;
+        if (s.skip != nullptr && tile.there) load_vec(s.skip, (uint64_t)tile.first, (uint64_t)slab.end, skip);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const float skip = s.skip != nullptr && tile.first + i < slab.end ? s.skip[tile.first + i] : 0.0f, x = (float)tile.x[i];
-            const float gb = du[tile.token][tile.wide + i][0], w = du[tile.token][tile.wide + i][1] * (1.0f / kLog2e);
-            dx[i] = __builtin_fmaf(gb, tile.d[i], skip * tile.dy[i]);
-            ddt[i] = __builtin_fmaf(gb, x, w);
-            if (s.softplus) ddt[i] *= sigmoid_of(tile.raw[i]);
-            const float y = __builtin_fmaf(skip, x, dys[tile.token][tile.wide + i]), z = (float)tile.gate[i], f = sigmoid_of(z);
-            dz[i] = (float)tile.dout[i] * y * __builtin_fmaf(z * f, 1.0f - f, f);
-            const bool inside = tile.there && t >= begin && t < finish;
-            if (!inside) dx[i] = ddt[i] = dz[i] = 0.0f;
-            to_skip[i] = inside ? tile.dy[i] * x : 0.0f;
-            to_bias[i] = ddt[i];
+            dx[i] = __builtin_fmaf(gb[i], tile.d[i], skip[i] * tile.dy[i]);
+            ddt[i] = __builtin_fmaf(gb[i], (float)tile.x[i], w[i] * (1.0f / kLog2e));
         }
+        if (s.softplus)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) ddt[i] *= sigmoid_of(tile.raw[i]);
+        if (!inside)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) dx[i] = ddt[i] = 0.0f;
+        // (each thread overwrites what only it has read)
+        float own[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) own[i] = inside ? tile.dy[i] * (float)tile.x[i] : 0.0f;
+        put_vec(ds[tile.token] + tile.wide, own);
+        put_vec(us[tile.token] + tile.wide, ddt);
         if (tile.there) {
             const uint64_t row = (slab.span * (uint64_t)s.span + t) * s.channels;
             store_vec(static_cast<T*>(g.dx) + row, tile.first, slab.end, dx);
             store_vec(static_cast<T*>(g.ddt) + row, tile.first, slab.end, ddt);
-            if (g.dgate != nullptr) store_vec(static_cast<T*>(g.dgate) + row, tile.first, slab.end, dz);
+            if (g.dgate != nullptr) {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    const float z = (float)tile.gate[i], f = sigmoid_of(z);
+                    y[i] = (float)tile.dout[i] * __builtin_fmaf(skip[i], (float)tile.x[i], y[i]) * __builtin_fmaf(z * f, 1.0f - f, f);
+                }
+                if (!inside)
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) y[i] = 0.0f;
+                store_vec(static_cast<T*>(g.dgate) + row, tile.first, slab.end, y);
+            }
         }
     }
     if (g.dskip == nullptr && g.dbias == nullptr) return;
-    // (each thread overwrites what only it has read)
-    if (tile.token < kTile)
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            du[tile.token][tile.wide + i][0] = to_skip[i];
-            du[tile.token][tile.wide + i][1] = to_bias[i];
-        }
     __syncthreads();
     for (uint32_t e = tid; e < 2 * kChannels; e += kScanThreads) {
+        const float* const from = e < kChannels ? &ds[0][e] : &us[0][e - kChannels];
         float v = 0.0f;
-        for (int j = 0; j < kTile; ++j) v += du[j][e / 2][e % 2];
-        g.means[(id * 2 + e % 2) * all + slab.padded + e / 2] = v;
+        for (int j = 0; j < kTile; ++j) v += from[j * kChannels];
+        g.means[(id * 2 + e / kChannels) * all + slab.padded + e % kChannels] = v;
     }
 }
 
