@@ -321,7 +321,7 @@ tcr_status tcr_causal_conv_step(const tcr_convolution *shape, const void *x, con
 /*
  * Gradients of tcr_causal_conv.  dout is laid out by o_stride; dx is contiguous (sequence, token, channel -- packed: token, channel) and not x or dout; dweight and
  * dbias (NULL: not wanted) like weight and bias, summed over all tokens, the same from run to run.  dfinal: the gradient of final_state (NULL: none), dstate:
- * of `state` (NULL: not wanted; neither's array).  Takes up to 2048 / ceil(channels / 256) sums of (width + 1) * channels floats of workspace and runs with one (with less
+ * of `state` (NULL: not wanted; neither's array).  Takes up to 1024 / ceil(channels / 256) sums of (width + 1) * channels floats of workspace and runs with one (with less
  * TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, as in tcr_rms_norm_backward).
  */
 tcr_status tcr_causal_conv_backward(const tcr_convolution *shape, const void *dout, const void *x, const void *weight, const void *bias, void *dx, void *dweight,
@@ -380,7 +380,7 @@ tcr_status tcr_selective_scan_backward(const tcr_selective *shape, const void *d
  * empty ones: 0.  An infinity or NaN among them makes the norm infinite or NaN, and what is scaled 0 (the infinity itself NaN) or NaN.
  * out: HOST array of `count` DEVICE pointers, where the scaled tensors go; NULL: in place.  Where the factor is 1, tensors in place are not written.  What is written
  * stands in no other tensor's place and only once in the list (TCR_ERR_INVALID_ARG).  max_norm, eps >= 0.  At most 2^40 elements.
- * Takes 16 KiB of workspace, or 8 bytes for each 120 tensors where that is more (with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded).
+ * Takes 64 KiB of workspace, or 8 bytes for each 143 tensors where that is more, less where the tensors are few and small (with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded).
  */
 typedef struct {
     void *data;

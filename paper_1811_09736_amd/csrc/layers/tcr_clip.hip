@@ -45,7 +45,11 @@ Launches tables_of(const tcr_tensor* tensors, void* const* out, uint64_t count) 
             got.tables.back().tensors = got.tables.back().pieces = 0;
         }
         ClipTable& table = got.tables.back();
-        table.tensor[table.tensors++] = {t.data, out != nullptr ? out[i] : t.data, t.count, table.pieces, t.dtype};
+        const uint32_t at = table.tensors++;
+        table.from[at] = t.data;
+        table.to[at] = out != nullptr ? out[i] : t.data;
+        table.count[at] = t.count << 2 | t.dtype;
+        table.first[at] = table.pieces;
         const uint32_t here = (uint32_t)div_up(t.count, kClipPiece);
         table.pieces += here;
         pieces += here;
@@ -62,7 +66,7 @@ Launches tables_of(const tcr_tensor* tensors, void* const* out, uint64_t count) 
 tcr_status sums_of(const Launches& l, double** sums, hipStream_t stream) {
     uint64_t got = 0;
     float* room = nullptr;
-    const uint64_t need = 2 * (uint64_t)std::max(l.parts, 1u);
+    const uint64_t need = 2 * ((uint64_t)l.parts + 1);             // (and one for all of them)
     const tcr_status st = partials_for(stream, need, need, &room, &got);
     if (st != TCR_OK) return st;
     *sums = reinterpret_cast<double*>(room);
@@ -76,7 +80,7 @@ tcr_status sums_of(const Launches& l, double** sums, hipStream_t stream) {
 }
 
 tcr_status norm_kernel(const Launches& l, const double* sums, float* norm, hipStream_t stream) {
-    clip_norm_kernel<<<dim3(1), kClipThreads, 0, stream>>>(sums, l.parts, norm);
+    clip_norm_kernel<<<dim3(1), kFoldThreads, 0, stream>>>(sums, l.parts, nullptr, norm);
     return launched("clip_norm_kernel");
 }
 
@@ -138,10 +142,18 @@ extern "C" tcr_status tcr_clip_gradients(const tcr_tensor* tensors, void* const*
         st = sums_of(l, &sums, s);
         if (st != TCR_OK) return st;
         if (l.tables.empty()) return norm_kernel(l, sums, norm, s);
+        const double* from = sums;
+        uint32_t parts = l.parts;
+        if (parts > kClipFew) {
+            clip_norm_kernel<<<dim3(1), kFoldThreads, 0, s>>>(sums, parts, sums + parts, norm);
+            if (launched("clip_norm_kernel") != TCR_OK) return TCR_ERR_HIP;
+            from += parts;
+            parts = 1;
+        }
         for (size_t i = 0; i < l.tables.size(); ++i) {
-            const ClipLimit limit = {max_norm, eps, i == 0 ? norm : nullptr};
+            const ClipLimit limit = {max_norm, eps, i == 0 && parts == l.parts ? norm : nullptr};
             const uint32_t blocks = std::min(l.tables[i].pieces, kClipParts);
-            clip_scale_kernel<<<dim3(blocks), kClipThreads, 0, s>>>(l.tables[i], limit, sums, l.parts);
+            clip_scale_kernel<<<dim3(blocks), kClipThreads, 0, s>>>(l.tables[i], limit, from, parts);
             if (launched("clip_scale_kernel") != TCR_OK) return TCR_ERR_HIP;
         }
         return TCR_OK;

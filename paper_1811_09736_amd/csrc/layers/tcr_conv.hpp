@@ -34,20 +34,24 @@ struct ConvGrad {
 
 template <typename T, int V> struct Some { typedef T v __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
 
-template <typename T, int V>
-__device__ __forceinline__ void load_some(const T* row, uint32_t col, uint32_t cols, float (&v)[V]) {
-    if (col + V <= cols) {
-        const typename Some<T, V>::v x = *reinterpret_cast<const typename Some<T, V>::v*>(row + col);
+// V elements as they are in memory.  WHOLE: the number of columns is a multiple of V, so that no vector goes beyond the end and no branch parts a load from the next.
+template <typename T, int V, bool WHOLE>
+__device__ __forceinline__ typename Some<T, V>::v raw_some(const T* row, uint32_t col, uint32_t cols) {
+    if (WHOLE || col + V <= cols) return *reinterpret_cast<const typename Some<T, V>::v*>(row + col);
+    typename Some<T, V>::v x;
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)x[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = col + i < cols ? (float)row[col + i] : 0.0f;
-    }
+    for (int i = 0; i < V; ++i) x[i] = col + i < cols ? row[col + i] : (T)0.0f;
+    return x;
 }
-template <typename T, int V>
+template <typename T, int V, bool WHOLE>
+__device__ __forceinline__ void load_some(const T* row, uint32_t col, uint32_t cols, float (&v)[V]) {
+    const typename Some<T, V>::v x = raw_some<T, V, WHOLE>(row, col, cols);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (float)x[i];
+}
+template <typename T, int V, bool WHOLE>
 __device__ __forceinline__ void store_some(T* row, uint32_t col, uint32_t cols, const float (&v)[V]) {
-    if (col + V <= cols) {
+    if (WHOLE || col + V <= cols) {
         typename Some<T, V>::v x;
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = (T)v[i];
@@ -60,36 +64,52 @@ __device__ __forceinline__ void store_some(T* row, uint32_t col, uint32_t cols, 
 }
 
 // The W - 1 inputs in front of token t of the sequence at `at`, the oldest first; those in front of the sequence from its state.
-template <typename T, int V, int W>
+template <typename T, int V, int W, bool WHOLE>
 __device__ __forceinline__ void load_front(const Conv& a, const T* x_row, const Place& at, uint32_t t, uint32_t col, float (&x)[W - 1][V]) {
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         const int64_t token = (int64_t)t - (W - 1) + j;
-        if (at.inside && token >= (int64_t)at.start) load_some(x_row + token * a.x_tok, col, a.channels, x[j]);
+        if (at.inside && token >= (int64_t)at.start) load_some<T, V, WHOLE>(x_row + token * a.x_tok, col, a.channels, x[j]);
         else if (at.inside && a.state != nullptr)
-            load_some(static_cast<const T*>(a.state) + ((uint64_t)at.seq * (W - 1) + (W - 1 + token - at.start)) * a.channels, col, a.channels, x[j]);
+            load_some<T, V, WHOLE>(static_cast<const T*>(a.state) + ((uint64_t)at.seq * (W - 1) + (W - 1 + token - at.start)) * a.channels, col, a.channels, x[j]);
         else
 #pragma unroll
             for (int i = 0; i < V; ++i) x[j][i] = 0.0f;
     }
 }
 // Rows of an array of states, [sequence][W - 1][channel].
-template <typename T, int V, int W>
+template <typename T, int V, int W, bool WHOLE>
 __device__ __forceinline__ void store_rows(void* states, uint64_t seq, const Conv& a, uint32_t col, const float (&x)[W - 1][V]) {
     if (states == nullptr) return;
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) store_some(static_cast<T*>(states) + (seq * (W - 1) + j) * a.channels, col, a.channels, x[j]);
+    for (int j = 0; j < W - 1; ++j) store_some<T, V, WHOLE>(static_cast<T*>(states) + (seq * (W - 1) + j) * a.channels, col, a.channels, x[j]);
 }
 
-template <typename T, int V, int W>
+// The taps of V channels, which lie behind one another: whole vectors where all of the channels are there.
+template <typename T, int V, int W, bool WHOLE>
 __device__ __forceinline__ void load_taps(const Conv& a, const T* weight, uint32_t col, float (&w)[W][V], float (&bias)[V]) {
+    const T* const from = weight + (uint64_t)col * W;
+    if (WHOLE || col + V <= a.channels) {
+        float flat[V * W];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const uint32_t c = col + i < a.channels ? col + i : a.channels - 1;
+        for (int j = 0; j < W; ++j) {
+            const typename Some<T, V>::v part = *reinterpret_cast<const typename Some<T, V>::v*>(from + j * V);
 #pragma unroll
-        for (int j = 0; j < W; ++j) w[j][i] = (float)weight[(uint64_t)c * W + j];
-        bias[i] = a.bias != nullptr ? (float)static_cast<const T*>(a.bias)[c] : 0.0f;
+            for (int i = 0; i < V; ++i) flat[j * V + i] = (float)part[i];
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j][i] = flat[i * W + j];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j][i] = col + i < a.channels ? (float)from[i * W + j] : 0.0f;
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) bias[i] = 0.0f;
+    if (a.bias != nullptr) load_some<T, V, WHOLE>(static_cast<const T*>(a.bias), col, a.channels, bias);
 }
 
 // What a thread works at: channels from col on, tokens t0 .. t1 - 1 of a span.
@@ -116,7 +136,7 @@ struct Part {
     }
 };
 
-template <typename T, int V, int W>
+template <typename T, int V, int W, bool WHOLE>
 __global__ __launch_bounds__(kConvThreads) void conv_kernel(Conv a) {
     Part my;
     if (!my.set(a, my.first<V>(a))) return;
@@ -124,12 +144,12 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(Conv a) {
     const T* const x_row = static_cast<const T*>(a.x) + my.span * a.x_seq;
     T* const out_row = static_cast<T*>(a.out) + my.span * a.out_seq;
     float w[W][V], bias[V], x[W][V];
-    load_taps<T, V, W>(a, static_cast<const T*>(a.weight), my.col, w, bias);
+    load_taps<T, V, W, WHOLE>(a, static_cast<const T*>(a.weight), my.col, w, bias);
     Place at;
     at.find(bounds, my.span, my.t0);
     {
         float front[W - 1][V];
-        load_front<T, V, W>(a, x_row, at, my.t0, my.col, front);
+        load_front<T, V, W, WHOLE>(a, x_row, at, my.t0, my.col, front);
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
 #pragma unroll
@@ -137,10 +157,9 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(Conv a) {
     }
     constexpr int kAhead = 4;
     for (uint32_t t = my.t0; t < my.t1; t += kAhead) {
-        float next[kAhead][V];
+        typename Some<T, V>::v next[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (t + u < my.t1) load_some(x_row + (t + u) * a.x_tok, my.col, a.channels, next[u]);
+        for (int u = 0; u < kAhead; ++u) next[u] = raw_some<T, V, WHOLE>(x_row + (t + u < my.t1 ? t + u : my.t1 - 1) * a.x_tok, my.col, a.channels);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (t + u >= my.t1) break;
@@ -150,9 +169,9 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(Conv a) {
                 for (int j = 0; j < W - 1; ++j)
 #pragma unroll
                     for (int i = 0; i < V; ++i) front[j][i] = x[j][i];
-                if (at.inside) store_rows<T, V, W>(a.fin, at.seq, a, my.col, front);
+                if (at.inside) store_rows<T, V, W, WHOLE>(a.fin, at.seq, a, my.col, front);
                 at.pass(bounds, t + u);
-                load_front<T, V, W>(a, x_row, at, t + u, my.col, front);
+                load_front<T, V, W, WHOLE>(a, x_row, at, t + u, my.col, front);
 #pragma unroll
                 for (int j = 0; j < W - 1; ++j)
 #pragma unroll
@@ -161,16 +180,21 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(Conv a) {
             float y[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                x[W - 1][i] = next[u][i];
+                x[W - 1][i] = (float)next[u][i];
                 float s = bias[i];
 #pragma unroll
                 for (int j = 0; j < W; ++j) s = __builtin_fmaf(w[j][i], x[j][i], s);
-                if (a.act) s *= sigmoid_of(s);
-                y[i] = at.inside ? s : 0.0f;
+                y[i] = s;
 #pragma unroll
                 for (int j = 0; j + 1 < W; ++j) x[j][i] = x[j + 1][i];
             }
-            store_some(out_row + (t + u) * a.out_tok, my.col, a.channels, y);
+            if (a.act)
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] *= sigmoid_of(y[i]);
+            if (!at.inside)
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = 0.0f;
+            store_some<T, V, WHOLE>(out_row + (t + u) * a.out_tok, my.col, a.channels, y);
         }
     }
     float front[W - 1][V];
@@ -179,19 +203,19 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(Conv a) {
         for (int j = 0; j < W - 1; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) front[j][i] = x[j][i];
-        store_rows<T, V, W>(a.fin, at.seq, a, my.col, front);
+        store_rows<T, V, W, WHOLE>(a.fin, at.seq, a, my.col, front);
     }
     if (a.offsets != nullptr && a.fin != nullptr)
         for (uint32_t e = my.run; e < bounds.count; e += a.runs)
             if (bounds.at(e + 1) <= bounds.at(e)) {
                 const Place empty = {e, 0, 0, true};
-                load_front<T, V, W>(a, x_row, empty, 0, my.col, front);
-                store_rows<T, V, W>(a.fin, e, a, my.col, front);
+                load_front<T, V, W, WHOLE>(a, x_row, empty, 0, my.col, front);
+                store_rows<T, V, W, WHOLE>(a.fin, e, a, my.col, front);
             }
 }
 
 // One token for every sequence.
-template <typename T, int V, int W>
+template <typename T, int V, int W, bool WHOLE>
 __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(Conv a) {
     const uint32_t cols = (a.channels + V - 1) / V;
     const uint64_t place = (uint64_t)workgroup() * kConvThreads + threadIdx.x, seq = place / cols;
@@ -199,9 +223,9 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(Conv a) {
     if (seq >= a.sequences) return;
     float w[W][V], bias[V], x[W][V], rows[W - 1][V], y[V];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) load_some(static_cast<const T*>(a.state) + (seq * (W - 1) + j) * a.channels, col, a.channels, x[j]);
-    load_some(static_cast<const T*>(a.x) + seq * a.x_seq, col, a.channels, x[W - 1]);
-    load_taps<T, V, W>(a, static_cast<const T*>(a.weight), col, w, bias);
+    for (int j = 0; j < W - 1; ++j) load_some<T, V, WHOLE>(static_cast<const T*>(a.state) + (seq * (W - 1) + j) * a.channels, col, a.channels, x[j]);
+    load_some<T, V, WHOLE>(static_cast<const T*>(a.x) + seq * a.x_seq, col, a.channels, x[W - 1]);
+    load_taps<T, V, W, WHOLE>(a, static_cast<const T*>(a.weight), col, w, bias);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         float s = bias[i];
@@ -211,11 +235,11 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(Conv a) {
 #pragma unroll
         for (int j = 0; j + 1 < W; ++j) rows[j][i] = x[j + 1][i];
     }
-    store_some(static_cast<T*>(a.out) + seq * a.out_seq, col, a.channels, y);
-    store_rows<T, V, W>(a.fin, seq, a, col, rows);
+    store_some<T, V, WHOLE>(static_cast<T*>(a.out) + seq * a.out_seq, col, a.channels, y);
+    store_rows<T, V, W, WHOLE>(a.fin, seq, a, col, rows);
 }
 
-template <typename T, int V, int W>
+template <typename T, int V, int W, bool WHOLE>
 __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
     __shared__ float sums[kConvThreads * V];
     const Conv& a = g.c;
@@ -233,10 +257,10 @@ __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
         const T* const dout_row = static_cast<const T*>(a.out) + my.span * a.out_seq;
         T* const dx_row = static_cast<T*>(g.dx) + (uint64_t)my.span * a.span * a.channels;
         float w[W][V], bias[V], x[W - 1][V], wait[W - 1][V];               // wait[m]: of the input at t - (W - 1) + m
-        load_taps<T, V, W>(a, static_cast<const T*>(a.weight), my.col, w, bias);
+        load_taps<T, V, W, WHOLE>(a, static_cast<const T*>(a.weight), my.col, w, bias);
         Place at;
         at.find(bounds, my.span, my.t0);
-        load_front<T, V, W>(a, x_row, at, my.t0, my.col, x);
+        load_front<T, V, W, WHOLE>(a, x_row, at, my.t0, my.col, x);
         auto clear = [&] {
 #pragma unroll
             for (int m = 0; m < W - 1; ++m)
@@ -247,9 +271,9 @@ __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
         auto put = [&](int64_t token, const float (&v)[V]) {
             if (!at.inside) return;
             if (token >= (int64_t)at.start) {
-                if (token >= (int64_t)my.t0 && token < (int64_t)my.t1) store_some(dx_row + token * a.channels, my.col, a.channels, v);
+                if (token >= (int64_t)my.t0 && token < (int64_t)my.t1) store_some<T, V, WHOLE>(dx_row + token * a.channels, my.col, a.channels, v);
             } else if (g.dstate != nullptr && at.start >= my.t0 && (at.start < my.t1 || a.span == 0)) {
-                store_some(static_cast<T*>(g.dstate) + ((uint64_t)at.seq * (W - 1) + (W - 1 + token - at.start)) * a.channels, my.col, a.channels, v);
+                store_some<T, V, WHOLE>(static_cast<T*>(g.dstate) + ((uint64_t)at.seq * (W - 1) + (W - 1 + token - at.start)) * a.channels, my.col, a.channels, v);
             }
         };
         // behind the last token of a sequence, at `end`: all that waits, and what comes from the state behind it
@@ -259,7 +283,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
             for (int m = 0; m < W - 1; ++m) {
                 if (g.dfinal != nullptr) {
                     float more[V];
-                    load_some(static_cast<const T*>(g.dfinal) + ((uint64_t)at.seq * (W - 1) + m) * a.channels, my.col, a.channels, more);
+                    load_some<T, V, WHOLE>(static_cast<const T*>(g.dfinal) + ((uint64_t)at.seq * (W - 1) + m) * a.channels, my.col, a.channels, more);
 #pragma unroll
                     for (int i = 0; i < V; ++i) wait[m][i] += more[i];
                 }
@@ -267,31 +291,11 @@ __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
             }
         };
         clear();
-        // (and the W - 1 tokens behind the run, whose gradients go to the run's last inputs)
-        for (uint32_t t = my.t0; t < my.t1 + (W - 1); ++t) {
-            if (t == at.next) {
-                finish(t);
-                if (t >= my.t1) break;
-                at.pass(bounds, t);
-                load_front<T, V, W>(a, x_row, at, t, my.col, x);
-                clear();
-            }
-            if (t >= a.span) break;
-            if (!at.inside && t >= my.t1) break;
-            float now[V], ds[V];
-            load_some(x_row + t * a.x_tok, my.col, a.channels, now);
-            load_some(dout_row + t * a.out_tok, my.col, a.channels, ds);
-            if (!at.inside) {
+        // one token: the slope, the sums (of the run's `own`), what it gives the inputs in front; `done` is the gradient of the input W - 1 tokens in front
+        auto token = [&](const float (&now)[V], float (&ds)[V], bool own, float (&done)[V]) {
+            if (a.act)
 #pragma unroll
-                for (int i = 0; i < V; ++i) ds[i] = 0.0f;
-                store_some(dx_row + (uint64_t)t * a.channels, my.col, a.channels, ds);
-                continue;
-            }
-            const bool own = t < my.t1;
-            float done[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (a.act) {
+                for (int i = 0; i < V; ++i) {
                     float s = bias[i];
 #pragma unroll
                     for (int j = 0; j < W - 1; ++j) s = __builtin_fmaf(w[j][i], x[j][i], s);
@@ -299,12 +303,16 @@ __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
                     const float z = sigmoid_of(s);
                     ds[i] *= __builtin_fmaf(s * z, 1.0f - z, z);
                 }
-                if (own) {
+            if (own)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
 #pragma unroll
                     for (int j = 0; j < W - 1; ++j) dw[j][i] = __builtin_fmaf(ds[i], x[j][i], dw[j][i]);
                     dw[W - 1][i] = __builtin_fmaf(ds[i], now[i], dw[W - 1][i]);
                     dw[W][i] += ds[i];
                 }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
 #pragma unroll
                 for (int m = 0; m < W - 1; ++m) wait[m][i] = __builtin_fmaf(w[m][i], ds[i], wait[m][i]);
                 done[i] = wait[0][i];
@@ -315,7 +323,48 @@ __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
                 for (int j = 0; j + 1 < W - 1; ++j) x[j][i] = x[j + 1][i];
                 x[W - 2][i] = now[i];
             }
-            put((int64_t)t - (W - 1), done);
+        };
+        // (and the W - 1 tokens behind the run, whose gradients go to the run's last inputs)
+        const uint32_t last = my.t1 + (W - 1);
+        for (uint32_t t = my.t0;;) {
+            if (at.inside) {
+                // as far as the sequence or the run goes: the loads of kAhead tokens ahead of their use
+                constexpr uint32_t kAhead = 4;
+                const uint32_t to = at.next < last ? at.next : last;
+                for (; t < to; t += kAhead) {
+                    typename Some<T, V>::v nows[kAhead], dss[kAhead];
+#pragma unroll
+                    for (uint32_t u = 0; u < kAhead; ++u) {
+                        const uint32_t from = t + u < to ? t + u : to - 1;
+                        nows[u] = raw_some<T, V, WHOLE>(x_row + from * a.x_tok, my.col, a.channels);
+                        dss[u] = raw_some<T, V, WHOLE>(dout_row + from * a.out_tok, my.col, a.channels);
+                    }
+#pragma unroll
+                    for (uint32_t u = 0; u < kAhead; ++u) {
+                        if (t + u >= to) break;
+                        float now[V], ds[V], done[V];
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            now[i] = (float)nows[u][i];
+                            ds[i] = (float)dss[u][i];
+                        }
+                        token(now, ds, t + u < my.t1, done);
+                        put((int64_t)(t + u) - (W - 1), done);
+                    }
+                }
+                t = to;
+                if (t != at.next) break;
+                finish(t);
+            } else {
+                float none[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) none[i] = 0.0f;
+                for (; t < my.t1 && t != at.next; ++t) store_some<T, V, WHOLE>(dx_row + (uint64_t)t * a.channels, my.col, a.channels, none);
+            }
+            if (t >= my.t1) break;
+            at.pass(bounds, t);
+            load_front<T, V, W, WHOLE>(a, x_row, at, t, my.col, x);
+            clear();
         }
         if (a.offsets != nullptr && g.dstate != nullptr)
             for (uint32_t e = my.run; e < bounds.count; e += a.runs)
@@ -323,8 +372,8 @@ __global__ __launch_bounds__(kConvThreads) void conv_grad_kernel(ConvGrad g) {
                     Conv of = a;
                     of.state = g.dfinal;
                     const Place empty = {e, 0, 0, true};
-                    load_front<T, V, W>(of, x_row, empty, 0, my.col, x);
-                    store_rows<T, V, W>(g.dstate, e, a, my.col, x);
+                    load_front<T, V, W, WHOLE>(of, x_row, empty, 0, my.col, x);
+                    store_rows<T, V, W, WHOLE>(g.dstate, e, a, my.col, x);
                 }
     }
     // the sums of the workgroup's runs, always in the same order

@@ -310,7 +310,7 @@ __device__ __forceinline__ void sum_shares(float (&v)[8], int lane) {
 }
 
 template <typename T, int P>
-__global__ __launch_bounds__(kScanThreads, 3) void selective_grad_kernel(SelectiveGrad g, uint32_t blocks) {
+__global__ __launch_bounds__(kScanThreads, P == 16 ? 2 : 3) void selective_grad_kernel(SelectiveGrad g, uint32_t blocks) {
     typedef GradTile<T, P> Tile;
     constexpr int K = 4, kWide = 64 / P, kTile = Tile::kTile, kStates = Tile::kStates, kChannels = Tile::kChannels, kTurns = kTile / kTurn;
     __shared__ __attribute__((aligned(16))) float ds[kTile][kChannels], us[kTile][kChannels];          // d, d x; then sum g b and sum g a exp(d a) h
