@@ -36,6 +36,7 @@ tcr_status run(Conv a, hipStream_t s) {
     cut(a, V);
     const uint64_t slabs = div_up(div_up(a.channels, V), a.lanes), blocks = slabs * div_up(spans_of(a) * a.runs, kConvThreads / a.lanes);
     if (blocks == 0) return TCR_OK;
+    if (blocks > 0xffffffffu) return TCR_ERR_UNSUPPORTED;
     if (a.channels % V == 0) conv_kernel<T, V, W, true><<<grid_of(blocks), kConvThreads, 0, s>>>(a);
     else conv_kernel<T, V, W, false><<<grid_of(blocks), kConvThreads, 0, s>>>(a);
     return launched("conv_kernel");
@@ -115,6 +116,7 @@ tcr_status forward(const tcr_convolution* shape, const void* x, const void* weig
     if (missing(weight, size) || !on_boundary(bias, size) || !on_boundary(state, size) || !on_boundary(last, size)) return TCR_ERR_INVALID_ARG;
     if (total_tokens(a) != 0) {
         if (missing(x, size) || missing(out, size)) return TCR_ERR_INVALID_ARG;
+        if (rows_meet(a, a.o_stride, a.channels)) return TCR_ERR_INVALID_ARG;
         // (the inputs in front of a run are another thread's)
         if (share(extent(a, out, a.o_stride, a.channels, size), extent(a, x, a.x_stride, a.channels, size))) return TCR_ERR_INVALID_ARG;
     }

@@ -40,7 +40,14 @@ Extent extent(const SHAPE& a, const void* p, const int64_t* stride, uint64_t wid
 // Whether two of them share memory for certain.  (Rows with gaps may stand in each other's; they are only looked at where they start.)
 inline bool share(const Extent& a, const Extent& b) { return a.whole && b.whole ? a.from < b.to && b.from < a.to : a.from == b.from; }
 
-// The same of two arrays without gaps, either of which may be missing.
+// Whether rows of `wide` elements that a call writes stand in each other's place for certain: steps from one to the next shorter than a row.
+template <typename SHAPE>
+bool rows_meet(const SHAPE& a, const int64_t* stride, uint64_t wide) {
+    auto shorter = [&](int64_t step) { return step < 0 ? (uint64_t)0 - (uint64_t)step < wide : (uint64_t)step < wide; };
+    return (a.offsets == nullptr && a.sequences > 1 && shorter(stride[0])) || (a.tokens > 1 && shorter(stride[1]));
+}
+
+// Whether two arrays without gaps share memory, either of which may be missing.
 inline bool arrays_share(const void* x, uint64_t x_bytes, const void* y, uint64_t y_bytes) {
     if (x == nullptr || y == nullptr) return false;
     const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);

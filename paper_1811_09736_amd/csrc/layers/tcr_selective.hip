@@ -28,6 +28,7 @@ tcr_status run(Selective s, hipStream_t stream) {
         if (s.per_span == 0) s.per_span = 1;
     };
     cut();
+    if (slabs * spans * s.per_span > kMostBlocks) return TCR_ERR_UNSUPPORTED;
     if (s.per_span > 1) {
         uint64_t got = 0;
         const tcr_status st = partials_for(stream, (s.per_span - 1) * each, 0, &s.ends, &got);
@@ -57,12 +58,18 @@ tcr_status run(const Selective& s, hipStream_t stream) {
     return run<T, 4, 16>(s, stream);
 }
 
+// Wavefronts from which on a thread takes two sequences: those that fill the chip.  4096 channels x 16 states, one / two / four: 32 sequences 6.9 / 6.9 / 8.8 us,
+// 256 sequences 43.5 / 34 / 36.5 us (143 MB).
+constexpr uint64_t kStepWaves = 2048;
+
 template <typename T, int P>
 tcr_status step(const Selective& s, hipStream_t stream) {
-    const uint32_t whole = s.states == 4 * P && on_boundary(s.state, 16) && on_boundary(s.fin, 16) && on_boundary(s.a, 16);
-    const uint64_t blocks = s.sequences * div_up(s.channels, kScanThreads / P);
+    const uint32_t whole = s.states == 4 * P && on_boundary(s.state, 16) && on_boundary(s.fin, 16);
+    const uint64_t slabs = div_up(s.channels, kScanThreads / P), blocks = s.sequences * slabs;
     if (blocks == 0) return TCR_OK;
-    selective_step_kernel<T, P><<<grid_of(blocks), kScanThreads, 0, stream>>>(s, whole);
+    if (blocks > kMostBlocks) return TCR_ERR_UNSUPPORTED;
+    if (blocks * (kScanThreads / 64) < kStepWaves) selective_step_kernel<T, P, 1><<<grid_of(blocks), kScanThreads, 0, stream>>>(s, whole);
+    else selective_step_kernel<T, P, 2><<<grid_of(slabs * div_up(s.sequences, 2)), kScanThreads, 0, stream>>>(s, whole);
     return launched("selective_step_kernel");
 }
 template <typename T>
@@ -83,6 +90,7 @@ tcr_status forward(const tcr_selective* shape, const void* x, const void* dt, co
     if (!on_boundary(state, 4) || !on_boundary(last, 4)) return TCR_ERR_INVALID_ARG;
     if (total_tokens(a) != 0) {
         if (missing(x, size) || missing(dt, size) || missing(b, size) || missing(c, size) || missing(out, size) || !on_boundary(gate, size)) return TCR_ERR_INVALID_ARG;
+        if (rows_meet(a, a.o_stride, a.channels)) return TCR_ERR_INVALID_ARG;
         // (other workgroups read what one has written out for: b and c, and in the states' kernel all of them)
         const Extent written = extent(a, out, a.o_stride, a.channels, size);
         if (share(written, extent(a, x, a.x_stride, a.channels, size)) || share(written, extent(a, dt, a.dt_stride, a.channels, size)) ||

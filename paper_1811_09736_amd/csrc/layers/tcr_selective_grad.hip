@@ -18,6 +18,7 @@ tcr_status run(SelectiveGrad g, hipStream_t stream) {
     s.length = kTile;
     s.per_span = s.span != 0 ? (uint32_t)div_up(s.span, kTile) : 1;
     const uint64_t slabs = (uint64_t)s.slabs * s.groups, all = slabs * kChannels, chunks = spans * s.per_span;
+    if (slabs * chunks > kMostBlocks) return TCR_ERR_UNSUPPORTED;
     // (all of it in front of the first launch: a call that lacks room has done nothing)
     const uint64_t sizes[] = {chunks * all * kStates, chunks * all * kStates, chunks * all, chunks * all * 2, slabs * tokens * 2 * kStates, chunks};
     uint64_t need = 0, got = 0;
@@ -36,7 +37,9 @@ tcr_status run(SelectiveGrad g, hipStream_t stream) {
         if (s.per_span > 1) {
             selective_parts_kernel<T, P><<<grid_of(blocks), kScanThreads, 0, stream>>>(g, (uint32_t)blocks);
             if (launched("selective_parts_kernel") != TCR_OK) return TCR_ERR_HIP;
-            selective_carry_kernel<kStates><<<dim3((unsigned)div_up(spans * all * kStates, 64), 2), 64 * kCarryLines, 0, stream>>>(g, all);
+            dim3 columns = grid_of(div_up(spans * all * kStates, 64));
+            columns.z = 2;
+            selective_carry_kernel<kStates><<<columns, 64 * kCarryLines, 0, stream>>>(g, all);
             if (launched("selective_carry_kernel") != TCR_OK) return TCR_ERR_HIP;
         }
         selective_grad_kernel<T, P><<<grid_of(blocks), kScanThreads, 0, stream>>>(g, (uint32_t)blocks);

@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
 
 // From chunks' own results to what reaches them: s.ends[i] becomes the state in front of chunk i, g.back[i] the gradient behind it.  A column of threads for each padded
 // channel and state, eight chunks a thread, a round of chunks for all of them: each thread makes one step of its eight, takes what the threads in front of it and the rounds before
-// bring, and goes over its eight again.  Forwards in the first row of workgroups, backwards in the second.  (64 chunks of 131072 columns 24 us, as many bytes as it has to move;
+// bring, and goes over its eight again.  Forwards in the first layer of workgroups, backwards in the second.  (64 chunks of 131072 columns 24 us, as many bytes as it has to move;
 // 96 chunks of 8192 columns, one thread a column from chunk to chunk: 37 us.)
 constexpr int kCarryLines = 8, kCarryChunks = 8;
 template <int NP>
@@ -198,14 +198,14 @@ __global__ __launch_bounds__(64 * kCarryLines) void selective_carry_kernel(Selec
     const Selective& s = g.s;
     const uint64_t spans = s.offsets != nullptr ? 1 : s.sequences, one = all * NP;
     const uint32_t lane = threadIdx.x % 64, line = threadIdx.x / 64;
-    const uint64_t at = (uint64_t)blockIdx.x * 64 + lane;
+    const uint64_t at = (uint64_t)workgroup() * 64 + lane;
     const bool real = at < spans * one;
     const uint64_t span = real ? at / one : 0, rest = real ? at % one : 0, padded = rest / NP;
     const uint32_t n = rest % NP;
     // (the channel that stands there)
     const uint64_t each = s.channels / s.groups, group_wide = all / s.groups, in_group = padded % group_wide, ch = padded / group_wide * each + in_group;
     const float rate = in_group < each && n < s.states ? s.a[ch * s.states + n] * kLog2e : 0.0f;
-    const bool backwards = blockIdx.y != 0;
+    const bool backwards = blockIdx.z != 0;
     float* const values = backwards ? g.back : s.ends;
     float carry = 0.0f;
     uint32_t turn = 0;

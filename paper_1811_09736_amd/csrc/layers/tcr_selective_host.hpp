@@ -8,6 +8,7 @@ namespace layers {
 
 constexpr uint64_t kMostTokens = 1ull << 31;       // in all; keeps every token index in range
 constexpr uint32_t kMostStates = 64, kMostChannels = 1u << 20;
+constexpr uint64_t kMostBlocks = 0xffffffffu;      // workgroups of a launch
 
 inline tcr_status check(const tcr_selective* a) {
     if (a == nullptr || a->dtype > TCR_F32 || a->channels == 0 || a->states == 0 || a->groups == 0 || a->channels % a->groups != 0 || a->softplus > 1)

@@ -64,6 +64,8 @@ def test_convolution_pointers():
         assert forward(conv(), **{name: BASE + 1}) == inv
     assert forward(conv(), out=BASE) == inv and forward(conv(), out=BASE + 128) == inv                  # x's place
     assert forward(conv(), state=FAR * 2, last=FAR * 2 + 64) == inv
+    for stride in ([640, 0], [640, 63], [640, -63], [32, 64], [0, 64]):                                 # rows of out in each other's place
+        assert forward(conv(o_stride=stride)) == inv and selective(scan(o_stride=stride)) == inv
     step = tcr.raw().tcr_causal_conv_step
     assert step(ctypes.byref(conv()), BASE, BASE, None, FAR, BASE, BASE, None) == inv                   # ten tokens
     assert step(ctypes.byref(conv(tokens=1)), BASE, BASE, None, FAR, None, BASE, None) == inv
