@@ -260,6 +260,22 @@ def test_gradients_packed(tcr, dtype, channels, states, groups, state, final):
         assert torch.equal(got["dstate"][0], dfinal[0])
 
 
+@pytest.mark.parametrize("bounds", [None, [0, 3, 600, 600, 601, 1100], [70, 1000]], ids=str)
+def test_gradients_over_many_chunks(tcr, bounds):
+    """1100 tokens in chunks of 8: more than the 64 that are carried in one round."""
+    lead = (1, 1100) if bounds is None else (1100,)
+    count = 1 if bounds is None else len(bounds) - 1
+    v = make(torch.float32, lead, 20, 3, state=count, seed=11)
+    offsets = None if bounds is None else torch.tensor(bounds, device="cuda")
+    dout, dfinal = torch.randn(*lead, 20, device="cuda"), torch.randn(count, 20, 3, device="cuda")
+    got = grads_of(tcr, v, dout, offsets, dfinal)
+    want, large = (reference(**v, softplus=True, offsets=offsets, dout=dout, dfinal=dfinal, large=m) for m in (False, True))
+    check_grads(got, want, large, 1100, 1100, v)
+    for name in ("dx", "ddt", "db", "dc", "dgate", "dstate"):
+        # errors of independent roundings that die out within some hundred tokens
+        assert (got[name].double() - want[name]).norm() <= 2.0 ** -19 * want[name].norm(), name
+
+
 def test_gradients_without_softplus(tcr):
     v = make(torch.float32, (2, 50), 24, 16, state=2, seed=5)
     v["dt"] = (v["dt"] * 0.2).contiguous()
