@@ -322,7 +322,7 @@ tcr_status tcr_causal_conv_step(const tcr_convolution *shape, const void *x, con
 /*
  * Gradients of tcr_causal_conv.  dout is laid out by o_stride; dx is contiguous (sequence, token, channel -- packed: token, channel) and not x or dout; dweight and
  * dbias (NULL: not wanted) like weight and bias, summed over all tokens, the same from run to run.  dfinal: the gradient of final_state (NULL: none), dstate:
- * of `state` (NULL: not wanted; neither's array).  Takes up to 1024 / ceil(channels / 256) sums of (width + 1) * channels floats of workspace and runs with one (with less
+ * of `state` (NULL: not wanted; neither's array).  Takes up to ceil(768 / ceil(channels / 256)) sums of (width + 1) * channels floats of workspace and runs with one (with less
  * TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, as in tcr_rms_norm_backward).
  */
 tcr_status tcr_causal_conv_backward(const tcr_convolution *shape, const void *dout, const void *x, const void *weight, const void *bias, void *dx, void *dweight,

@@ -15,17 +15,19 @@ constexpr uint32_t kMostChannels = 1u << 20;
 // Threads that a call is cut for, and tokens of a run at most (the W - 1 in front of it are loaded once more).
 constexpr uint64_t kFillThreads = 1u << 18;
 constexpr uint32_t kLongRun = 32, kShortRun = 4;
-// Workgroups of the gradients: four for each compute unit (8191 tokens x 4096 channels: 68 us, eight 70).
-constexpr uint64_t kGradBlocks = 1024;
+// Workgroups of the gradients: three for each compute unit, which are there at once (165 registers), each with runs as long as it takes.  8191 tokens x 4096 channels: 55 us, and 5 for the
+// sums; with four workgroups, of which one waits for the others, 62 and 6.
+constexpr uint64_t kGradBlocks = 768;
 
 uint64_t spans_of(const Conv& a) { return a.offsets != nullptr ? 1 : a.sequences; }
 
-void cut(Conv& a, int vec) {
+void cut(Conv& a, int vec, uint64_t threads, uint64_t longest) {
     const uint64_t cols = div_up(a.channels, vec);
     a.lanes = 64;
     while (a.lanes > 1 && a.lanes / 2 >= cols) a.lanes /= 2;
-    uint64_t run = spans_of(a) * a.span * cols / kFillThreads / kShortRun * kShortRun;
-    a.run = run < kShortRun ? kShortRun : run > kLongRun ? kLongRun : (uint32_t)run;
+    uint64_t run = div_up(spans_of(a) * a.span * cols, threads);
+    if (run > longest) run = longest;
+    a.run = run < kShortRun ? kShortRun : (uint32_t)run;
     a.runs = (uint32_t)div_up(a.span, a.run);
     if (a.runs == 0) a.runs = 1;
 }
@@ -33,7 +35,7 @@ void cut(Conv& a, int vec) {
 template <typename T, int W>
 tcr_status run(Conv a, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
-    cut(a, V);
+    cut(a, V, kFillThreads, kLongRun);
     const uint64_t slabs = div_up(div_up(a.channels, V), a.lanes), blocks = slabs * div_up(spans_of(a) * a.runs, kConvThreads / a.lanes);
     if (blocks == 0) return TCR_OK;
     if (blocks > 0xffffffffu) return TCR_ERR_UNSUPPORTED;
@@ -55,7 +57,7 @@ tcr_status step(Conv a, hipStream_t s) {
 template <typename T, int W>
 tcr_status gradients(ConvGrad g, T* dweight, T* dbias, hipStream_t s) {
     constexpr int V = 4;
-    cut(g.c, V);
+    cut(g.c, V, kGradBlocks * kConvThreads, kMostTokens);
     const uint64_t slabs = div_up(div_up(g.c.channels, V), g.c.lanes), places = div_up(spans_of(g.c) * g.c.runs, kConvThreads / g.c.lanes);
     const uint64_t each = (uint64_t)(W + 1) * g.c.channels;
     uint64_t parts = div_up(kGradBlocks, slabs), got = 0;
