@@ -129,21 +129,22 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
         pass[k] = 1.0f;
     }
     bool open = at.start != t0;                // whether what comes back from here reaches the tokens in front of the chunk
-    if (!open)
-#pragma unroll
-        for (int k = 0; k < K; ++k) pass[k] = 0.0f;
     if (at.inside && at.start == t0) load_states(s.state, at.seq, s, ch, n0, real, h);
     __syncthreads();
     float sum = 0.0f;
-    auto token = [&](uint32_t j) {
-        const float d = ds[j][wide], u = us[j][wide], dy = dys[j][wide];
+    // BACK: with what comes back -- not from behind a bound, where another sequence may hold infinities or NaN that no factor of 0 would keep there.
+    auto token = [&](auto with_back, uint32_t j) {
+        constexpr bool BACK = decltype(with_back)::value;
+        const float d = ds[j][wide], u = us[j][wide], dy = BACK ? dys[j][wide] : 0.0f;
         sum += d;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const float a = __builtin_amdgcn_exp2f(d * rate[k]);
             h[k] = __builtin_fmaf(a, h[k], u * bs[j][n0 + k]);
-            pass[k] *= a;
-            back[k] = __builtin_fmaf(pass[k], cs[j][n0 + k] * dy, back[k]);
+            if (BACK) {
+                pass[k] *= a;
+                back[k] = __builtin_fmaf(pass[k], cs[j][n0 + k] * dy, back[k]);
+            }
         }
     };
     auto leave = [&] {                         // the sequence ends here
@@ -158,8 +159,12 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
     for (uint32_t j = 0; j < here; j += kTokens) {
         const uint32_t t = t0 + j;
         if (at.next >= t + kTokens || at.next >= t1) {
+            if (open)
 #pragma unroll
-            for (int i = 0; i < kTokens; ++i) token(j + i);
+                for (int i = 0; i < kTokens; ++i) token(std::true_type(), j + i);
+            else
+#pragma unroll
+                for (int i = 0; i < kTokens; ++i) token(std::false_type(), j + i);
             continue;
         }
         for (uint32_t i = 0; i < kTokens && t + i < t1; ++i) {
@@ -168,10 +173,11 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
                 open = false;
                 at.pass(bounds, t + i);
 #pragma unroll
-                for (int k = 0; k < K; ++k) h[k] = pass[k] = 0.0f;
+                for (int k = 0; k < K; ++k) h[k] = 0.0f;
                 if (at.inside) load_states(s.state, at.seq, s, ch, n0, real, h);
             }
-            token(j + i);
+            if (open) token(std::true_type(), j + i);
+            else token(std::false_type(), j + i);
         }
     }
     if (at.next == t1) leave();
