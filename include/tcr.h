@@ -345,7 +345,8 @@ tcr_status tcr_causal_conv_backward(const tcr_convolution *shape, const void *do
  * 1 <= states <= 64, channels <= 2^20, a multiple of groups; fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED beyond).  An infinity or NaN of a token stays in its
  * sequence, from that token on, and in its channel (of b and c: its group).
  * Results are the same from run to run.  Workspace: where sequences and channels are too few to fill the chip, tokens are cut into chunks whose states pass through it,
- * 64 chunks of a sequence at most; with less of it, or none, the call takes fewer chunks and longer, and its sums other roundings.
+ * 64 chunks of a sequence at most; with less of it, or none, the call takes fewer chunks and longer, and its sums other roundings.  Factors above 1 (a of the sign of d) are as good
+ * as others while the states stay in binary32's range, whatever their product over a chunk.
  */
 typedef struct {
     uint32_t dtype, channels, states, groups, softplus;

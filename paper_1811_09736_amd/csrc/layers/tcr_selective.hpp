@@ -48,6 +48,11 @@ __device__ __forceinline__ float log1p_unit(float e) {
 // (the median of x, 0 and infinity is the larger of x and 0 in one operation, and no NaN: a NaN comes by way of the logarithm)
 __device__ __forceinline__ float softplus_of(float x) { return __builtin_amdgcn_fmed3f(x, 0.0f, __builtin_inff()) + log1p_unit(exp_of(-__builtin_fabsf(x))); }
 
+// A value h carried over many tokens at once, whose steps sum to `sum`: 2^(sum rate) h + end.  Both may be in range where the factor is not, so it is applied in three equal parts:
+// third_of is one of them.  Its limit of 2^127 keeps 0 at 0 and takes nothing else away: 2^381 h is beyond the range for every other h.
+__device__ __forceinline__ float third_of(float sum, float third_rate) { return __builtin_amdgcn_exp2f(__builtin_fminf(sum * third_rate, 127.0f)); }
+__device__ __forceinline__ float carried(float third, float h, float end) { return __builtin_fmaf(third, third * (third * h), end); }
+
 // The states n0 .. n0 + K - 1 of a channel in an array [sequence][channel][state]; 0 where there is no array or no such state.
 template <int K>
 __device__ __forceinline__ void load_states(const float* states, uint64_t seq, const Selective& s, uint32_t ch, uint32_t n0, bool real, float (&h)[K]) {
@@ -162,7 +167,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_kernel(Selective s, ui
     Place at;
     at.find(bounds, slab.span, t0);
 
-    float rate[K], h[K], sum = 0.0f;
+    float rate[K], h[K], sum = 0.0f, total = 0.0f;         // sums of d: of a tile, of the chunk (in two levels: the factor over a chunk has the sum in its exponent)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         rate[k] = real && n0 + k < s.states ? s.a[(uint64_t)ch * s.states + n0 + k] * kLog2e : 0.0f;
@@ -179,7 +184,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_kernel(Selective s, ui
         for (++i; i < slab.chunk; ++i) {
             const float passed = s.sums[i * one + place];
 #pragma unroll
-            for (int k = 0; k < K; ++k) h[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(passed * rate[k]), h[k], end_of(i, k));
+            for (int k = 0; k < K; ++k) h[k] = carried(third_of(passed, rate[k] * (1.0f / 3.0f)), h[k], end_of(i, k));
         }
     }
 
@@ -286,6 +291,10 @@ __global__ __launch_bounds__(kScanThreads) void selective_kernel(Selective s, ui
             }
         }
         __syncthreads();
+        if (!OUT) {
+            total += sum;
+            sum = 0.0f;
+        }
         const uint32_t t = tile + my_token;
         if (OUT && t < t1 && my_first < my_end) {
             get_vec(ds[my_token] + my_wide, v);
@@ -315,7 +324,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_kernel(Selective s, ui
         const uint64_t place = (slab.chunk * spans + slab.span) * all + slab.padded + wide;
 #pragma unroll
         for (int k = 0; k < K; ++k) s.ends[place * kStates + n0 + k] = h[k];
-        if (lane < kWide) s.sums[place] = sum;
+        if (lane < kWide) s.sums[place] = total;
     }
 }
 

@@ -6,7 +6,7 @@
 //     da[n] = sum_t g_t[n] d_t exp(d_t a[n]) h_{t-1}[n],   dskip = sum_t dy_t x_t,   ddt_t = dd_t sigmoid(dt_t + bias),   dbias = sum_t ddt_t.
 //
 // Tokens are cut into chunks of one tile.  selective_parts_kernel goes over them once: a chunk's state from nothing and, with the product of the factors so far, what it
-// hands back to the tokens in front of it.  selective_carry_kernel makes of these the states in front of every chunk and the gradients behind it.  selective_grad_kernel
+// hands back to the tokens in front of it (where factors may be above 1 once more, backwards).  selective_carry_kernel makes of these the states in front of every chunk and the gradients behind it.  selective_grad_kernel
 // then does every chunk by itself: forwards once more with the states in front of each kTurn tokens kept in LDS, then turn by turn from the last to the first, the turn's
 // states and factors in registers.  Sums over channels and over chunks pass through the workspace and are added up in the same order every time.
 // What bounds it is the vector unit: two exponentials and about twenty operations for each state and token.
@@ -106,6 +106,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
     typedef GradTile<T, P> Tile;
     constexpr int K = 4, kWide = 64 / P, kTile = Tile::kTile, kStates = Tile::kStates, kChannels = Tile::kChannels;
     __shared__ __attribute__((aligned(16))) float ds[kTile][kChannels], us[kTile][kChannels], dys[kTile][kChannels], bs[kTile][kStates], cs[kTile][kStates];
+    __shared__ bool grown[4];
     if (workgroup() >= blocks) return;
     const Selective& s = g.s;
     const Slab<P> slab(s, s.per_span);
@@ -116,21 +117,31 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
     const uint32_t begin = s.offsets != nullptr ? bounds.at(0) : 0, finish = s.offsets != nullptr ? bounds.at(bounds.count) : s.span;
     Place at;
     at.find(bounds, slab.span, t0);
+    bool grows = false;
     {
         Tile tile;
         tile.load(g, slab, t0, t1, begin, finish);
         tile.put(g, slab, t0, t1, begin, finish, ds, us, dys, bs, cs);
+        if (!s.softplus)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) grows |= tile.d[i] < 0.0f;
     }
     float rate[K], h[K], pass[K], back[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         rate[k] = real && n0 + k < s.states ? s.a[(uint64_t)ch * s.states + n0 + k] * kLog2e : 0.0f;
+        grows |= rate[k] > 0.0f;
         h[k] = back[k] = 0.0f;
         pass[k] = 1.0f;
     }
+    if (__any(grows) && lane == 0) grown[threadIdx.x >> 6] = true;
+    else if (lane == 0) grown[threadIdx.x >> 6] = false;
     bool open = at.start != t0;                // whether what comes back from here reaches the tokens in front of the chunk
     if (at.inside && at.start == t0) load_states(s.state, at.seq, s, ch, n0, real, h);
     __syncthreads();
+    // Where a factor may be above 1, products of factors leave the range though nothing that they carry does: what comes back is made by itself, from the last token to the first.
+    // (Twice the exponentials.  Factors of at most 1 only vanish, and what they carry with them.)
+    grows = grown[0] | grown[1] | grown[2] | grown[3];
     float sum = 0.0f;
     // BACK: with what comes back -- not from behind a bound, where another sequence may hold infinities or NaN that no factor of 0 would keep there.
     auto token = [&](auto with_back, uint32_t j) {
@@ -148,7 +159,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
         }
     };
     auto leave = [&] {                         // the sequence ends here
-        if (open && at.inside && g.dfinal != nullptr) {
+        if (open && !grows && at.inside && g.dfinal != nullptr) {
             float after[K];
             load_states(g.dfinal, at.seq, s, ch, n0, real, after);
 #pragma unroll
@@ -159,7 +170,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
     for (uint32_t j = 0; j < here; j += kTokens) {
         const uint32_t t = t0 + j;
         if (at.next >= t + kTokens || at.next >= t1) {
-            if (open)
+            if (open && !grows)
 #pragma unroll
                 for (int i = 0; i < kTokens; ++i) token(std::true_type(), j + i);
             else
@@ -176,11 +187,22 @@ __global__ __launch_bounds__(kScanThreads) void selective_parts_kernel(Selective
                 for (int k = 0; k < K; ++k) h[k] = 0.0f;
                 if (at.inside) load_states(s.state, at.seq, s, ch, n0, real, h);
             }
-            if (open) token(std::true_type(), j + i);
+            if (open && !grows) token(std::true_type(), j + i);
             else token(std::false_type(), j + i);
         }
     }
     if (at.next == t1) leave();
+    if (grows) {
+        at.find(bounds, slab.span, t0);
+        if (at.start != t0) {
+            if (at.inside && at.next <= t1) load_states(g.dfinal, at.seq, s, ch, n0, real, back);
+            for (uint32_t j = (at.next < t1 ? at.next : t1) - t0; j-- > 0;) {
+                const float d = ds[j][wide], dy = dys[j][wide];
+#pragma unroll
+                for (int k = 0; k < K; ++k) back[k] = __builtin_amdgcn_exp2f(d * rate[k]) * __builtin_fmaf(cs[j][n0 + k], dy, back[k]);
+            }
+        }
+    }
     const uint64_t spans = s.offsets != nullptr ? 1 : s.sequences, all = (uint64_t)s.slabs * s.groups * kChannels, id = slab.chunk * spans + slab.span;
     const uint64_t place = id * all + slab.padded + wide;
 #pragma unroll
@@ -210,7 +232,7 @@ __global__ __launch_bounds__(64 * kCarryLines) void selective_carry_kernel(Selec
     const uint32_t n = rest % NP;
     // (the channel that stands there)
     const uint64_t each = s.channels / s.groups, group_wide = all / s.groups, in_group = padded % group_wide, ch = padded / group_wide * each + in_group;
-    const float rate = in_group < each && n < s.states ? s.a[ch * s.states + n] * kLog2e : 0.0f;
+    const float rate = in_group < each && n < s.states ? s.a[ch * s.states + n] * (kLog2e / 3.0f) : 0.0f;     // (a third)
     const bool backwards = blockIdx.z != 0;
     float* const values = backwards ? g.back : s.ends;
     float carry = 0.0f;
@@ -231,30 +253,30 @@ __global__ __launch_bounds__(64 * kCarryLines) void selective_carry_kernel(Selec
             keep[i] = s.sums[id * all + padded];
             open[i] = g.closed == nullptr || g.closed[id] == 0;
         }
-        float step = 1.0f, sum = 0.0f;
+        float step = 0.0f, sum = 0.0f;         // step: the sum of d
         bool shut = false;
 #pragma unroll
         for (int i = 0; i < kCarryChunks; ++i) {
-            keep[i] = __builtin_amdgcn_exp2f(rate * keep[i]);
+            if (first + i < s.per_span) step += keep[i];
+            keep[i] = third_of(keep[i], rate);
             if (first + i >= s.per_span) break;
-            sum = open[i] ? __builtin_fmaf(keep[i], sum, v[i]) : v[i];
-            step *= keep[i];
+            sum = open[i] ? carried(keep[i], sum, v[i]) : v[i];
             shut |= !open[i];
         }
-        steps[turn][line][lane] = step;
+        steps[turn][line][lane] = third_of(step, rate);
         sums[turn][line][lane] = sum;
         closed[turn][line][lane] = shut;
         __syncthreads();
         float mine = carry;
         for (uint32_t l = 0; l < kCarryLines; ++l) {
             if (l == line) mine = carry;
-            carry = closed[turn][l][lane] ? sums[turn][l][lane] : __builtin_fmaf(steps[turn][l][lane], carry, sums[turn][l][lane]);
+            carry = closed[turn][l][lane] ? sums[turn][l][lane] : carried(steps[turn][l][lane], carry, sums[turn][l][lane]);
         }
 #pragma unroll
         for (int i = 0; i < kCarryChunks; ++i) {
             if (first + i >= s.per_span) break;
             if (real) values[id_of(i) * one + rest] = mine;
-            mine = open[i] ? __builtin_fmaf(keep[i], mine, v[i]) : v[i];
+            mine = open[i] ? carried(keep[i], mine, v[i]) : v[i];
         }
     }
 }
