@@ -3,6 +3,7 @@
 #include <exception>
 #include <type_traits>
 
+#include "tcr_lattice.hpp"
 #include "tcr_shared.hpp"
 
 namespace tcr {
@@ -40,11 +41,10 @@ Extent extent(const SHAPE& a, const void* p, const int64_t* stride, uint64_t wid
 // Whether two of them share memory for certain.  (Rows with gaps may stand in each other's; they are only looked at where they start.)
 inline bool share(const Extent& a, const Extent& b) { return a.whole && b.whole ? a.from < b.to && b.from < a.to : a.from == b.from; }
 
-// Whether rows of `wide` elements that a call writes stand in each other's place for certain: steps from one to the next shorter than a row.
+// Whether rows of `wide` elements that a call writes share elements with each other.
 template <typename SHAPE>
 bool rows_meet(const SHAPE& a, const int64_t* stride, uint64_t wide) {
-    auto shorter = [&](int64_t step) { return step < 0 ? (uint64_t)0 - (uint64_t)step < wide : (uint64_t)step < wide; };
-    return (a.offsets == nullptr && a.sequences > 1 && shorter(stride[0])) || (a.tokens > 1 && shorter(stride[1]));
+    return lattice_meets(a.offsets == nullptr ? a.sequences : 1, a.offsets == nullptr ? stride[0] : 0, a.tokens, stride[1], wide);
 }
 
 // Whether two arrays without gaps share memory, either of which may be missing.
