@@ -382,7 +382,8 @@ tcr_status tcr_selective_scan_backward(const tcr_selective *shape, const void *d
  * empty ones: 0.  An infinity or NaN among them makes the norm infinite or NaN, and what is scaled 0 (the infinity itself NaN) or NaN.
  * out: HOST array of `count` DEVICE pointers, where the scaled tensors go; NULL: in place.  Where the factor is 1, tensors in place are not written.  What is written
  * stands in no other tensor's place and only once in the list (TCR_ERR_INVALID_ARG).  max_norm, eps >= 0.  At most 2^40 elements.
- * Takes 64 KiB of workspace, or 8 bytes for each 143 tensors where that is more, less where the tensors are few and small (with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded).
+ * Takes 64 KiB of workspace, or 8 bytes for each 143 tensors where that is more, less where the tensors are few and small; of a caller's buffer that is the second half of what follows its
+ * first 256 bytes (with less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, and nothing done).
  */
 typedef struct {
     void *data;

@@ -54,9 +54,10 @@ Launches tables_of(const tcr_tensor* tensors, void* const* out, uint64_t count) 
         table.pieces += here;
         pieces += here;
     }
-    // (all launches together have kClipParts sums, or one each)
+    // (all launches together have kClipParts sums at most, or one each: one, and a share of the others)
+    const uint64_t launches = got.tables.size(), more = launches < kClipParts ? kClipParts - launches : 0;
     for (const ClipTable& t : got.tables) {
-        const uint64_t share = pieces <= kClipParts ? t.pieces : std::max<uint64_t>(1, (uint64_t)t.pieces * kClipParts / pieces);
+        const uint64_t share = pieces <= kClipParts ? t.pieces : 1 + (uint64_t)(t.pieces - 1) * more / (pieces - launches + (more == 0));
         got.blocks.push_back((uint32_t)share);
         got.parts += (uint32_t)share;
     }
@@ -66,7 +67,7 @@ Launches tables_of(const tcr_tensor* tensors, void* const* out, uint64_t count) 
 tcr_status sums_of(const Launches& l, double** sums, hipStream_t stream) {
     uint64_t got = 0;
     float* room = nullptr;
-    const uint64_t need = 2 * ((uint64_t)l.parts + 1);             // (and one for all of them)
+    const uint64_t need = 2 * (uint64_t)l.parts;
     const tcr_status st = partials_for(stream, need, need, &room, &got);
     if (st != TCR_OK) return st;
     *sums = reinterpret_cast<double*>(room);
@@ -142,18 +143,16 @@ extern "C" tcr_status tcr_clip_gradients(const tcr_tensor* tensors, void* const*
         st = sums_of(l, &sums, s);
         if (st != TCR_OK) return st;
         if (l.tables.empty()) return norm_kernel(l, sums, norm, s);
-        const double* from = sums;
         uint32_t parts = l.parts;
         if (parts > kClipFew) {
-            clip_norm_kernel<<<dim3(1), kFoldThreads, 0, s>>>(sums, parts, sums + parts, norm);
+            clip_norm_kernel<<<dim3(1), kFoldThreads, 0, s>>>(sums, parts, sums, norm);
             if (launched("clip_norm_kernel") != TCR_OK) return TCR_ERR_HIP;
-            from += parts;
             parts = 1;
         }
         for (size_t i = 0; i < l.tables.size(); ++i) {
             const ClipLimit limit = {max_norm, eps, i == 0 && parts == l.parts ? norm : nullptr};
             const uint32_t blocks = std::min(l.tables[i].pieces, kClipParts);
-            clip_scale_kernel<<<dim3(blocks), kClipThreads, 0, s>>>(l.tables[i], limit, from, parts);
+            clip_scale_kernel<<<dim3(blocks), kClipThreads, 0, s>>>(l.tables[i], limit, sums, parts);
             if (launched("clip_scale_kernel") != TCR_OK) return TCR_ERR_HIP;
         }
         return TCR_OK;

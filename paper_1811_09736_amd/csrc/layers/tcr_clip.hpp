@@ -95,7 +95,7 @@ __device__ __forceinline__ double total_of(const double* sums, uint32_t parts, d
     return block_sum<THREADS>(v, room);
 }
 
-// One sum of all of them (total: NULL: not wanted), and the norm (likewise).
+// One sum of all of them (total: NULL: not wanted; may be `sums`, all of which is read in front of it), and the norm (NULL: likewise).
 __global__ __launch_bounds__(kFoldThreads) void clip_norm_kernel(const double* sums, uint32_t parts, double* total, float* norm) {
     __shared__ double room[kFoldThreads / 64];
     const double v = total_of<kFoldThreads>(sums, parts, room);
