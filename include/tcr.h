@@ -303,8 +303,8 @@ tcr_status tcr_rms_norm_backward(const void *dout, const void *total, const void
  * starts b * stride[0] + t * stride[1] ELEMENTS behind the pointer.  weight: channels x width elements, bias: `channels` (NULL: zeros).  All of dtype; element
  * alignment is enough.  Arithmetic is binary32, rounded once.  offsets: as in tcr_linear_attention, with 0 in rows of out whose token lies in no sequence.
  * state, final_state: sequences x (width - 1) x channels elements, contiguous: the inputs in front of the first token and the last ones, the oldest
- * first (with fewer tokens than width - 1 the state's own among them).  NULL: zeros, and not wanted.  They must be different arrays, out not x, and no two rows of out
- * may share elements (TCR_ERR_INVALID_ARG).
+ * first (with fewer tokens than width - 1 the state's own among them).  NULL: zeros, and not wanted.  They must be different arrays, neither of them out,
+ * final_state and out not x (TCR_ERR_INVALID_ARG where rows without gaps show it, or equal first rows), and no two rows of out may share elements (TCR_ERR_INVALID_ARG).
  * 2 <= width <= 4, channels <= 2^20, fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED beyond).  No workspace.
  */
 typedef struct {
@@ -340,8 +340,8 @@ tcr_status tcr_causal_conv_backward(const tcr_convolution *shape, const void *do
  *   offsets == NULL: `sequences` sequences of `tokens` tokens each; otherwise packed ones, as in tcr_linear_attention.  Rows of out whose token lies in
  *   no sequence are set to 0.
  * state, final_state: DEVICE pointers, sequences x channels x states floats each, contiguous; the states in front of the first token and behind the last
- * (of an empty sequence: the same).  NULL: zeros, and not wanted.  They must be different arrays, out none of the inputs (TCR_ERR_INVALID_ARG where rows
- * without gaps show it, or equal first rows), and no two of its rows may share elements (TCR_ERR_INVALID_ARG).
+ * (of an empty sequence: the same).  NULL: zeros, and not wanted.  They must be different arrays, neither of them out, final_state and out none of the inputs
+ * (TCR_ERR_INVALID_ARG where rows without gaps show it, or equal first rows), and no two of its rows may share elements (TCR_ERR_INVALID_ARG).
  * 1 <= states <= 64, channels <= 2^20, a multiple of groups; fewer than 2^31 tokens in all (TCR_ERR_UNSUPPORTED beyond).  An infinity or NaN of a token stays in its
  * sequence, from that token on, and in its channel (of b and c: its group).
  * Results are the same from run to run.  Workspace: where sequences and channels are too few to fill the chip, tokens are cut into chunks whose states pass through it,

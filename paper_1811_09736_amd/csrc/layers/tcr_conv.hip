@@ -119,8 +119,10 @@ tcr_status forward(const tcr_convolution* shape, const void* x, const void* weig
     if (total_tokens(a) != 0) {
         if (missing(x, size) || missing(out, size)) return TCR_ERR_INVALID_ARG;
         if (rows_meet(a, a.o_stride, a.channels)) return TCR_ERR_INVALID_ARG;
-        // (the inputs in front of a run are another thread's)
-        if (share(extent(a, out, a.o_stride, a.channels, size), extent(a, x, a.x_stride, a.channels, size))) return TCR_ERR_INVALID_ARG;
+        // (the inputs in front of a run are another thread's, and so are the states)
+        const Extent written = extent(a, out, a.o_stride, a.channels, size), read = extent(a, x, a.x_stride, a.channels, size);
+        if (share(written, read) || share(written, state, state_bytes(a)) || share(written, last, state_bytes(a))) return TCR_ERR_INVALID_ARG;
+        if (!one && share(read, last, state_bytes(a))) return TCR_ERR_INVALID_ARG;
     }
     if ((state != last || !one) && arrays_share(state, state_bytes(a), last, state_bytes(a))) return TCR_ERR_INVALID_ARG;
     Conv c = arguments(a, x, weight, bias, state);

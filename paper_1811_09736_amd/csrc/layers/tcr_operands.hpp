@@ -40,6 +40,11 @@ Extent extent(const SHAPE& a, const void* p, const int64_t* stride, uint64_t wid
 }
 // Whether two of them share memory for certain.  (Rows with gaps may stand in each other's; they are only looked at where they start.)
 inline bool share(const Extent& a, const Extent& b) { return a.whole && b.whole ? a.from < b.to && b.from < a.to : a.from == b.from; }
+// An array without gaps against it; either may be missing or empty.
+inline bool share(const Extent& a, const void* p, uint64_t bytes) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+    return p != nullptr && bytes != 0 && share(a, Extent{from, from + (uintptr_t)bytes, true});
+}
 
 // Whether rows of `wide` elements that a call writes share elements with each other.
 template <typename SHAPE>

@@ -88,17 +88,17 @@ tcr_status forward(const tcr_selective* shape, const void* x, const void* dt, co
     const tcr_selective& a = *shape;
     const uintptr_t size = a.dtype == TCR_F32 ? 4 : 2;
     if (!on_boundary(state, 4) || !on_boundary(last, 4)) return TCR_ERR_INVALID_ARG;
+    const uint64_t bytes = 4 * a.sequences * (uint64_t)a.channels * a.states;
     if (total_tokens(a) != 0) {
         if (missing(x, size) || missing(dt, size) || missing(b, size) || missing(c, size) || missing(out, size) || !on_boundary(gate, size)) return TCR_ERR_INVALID_ARG;
         if (rows_meet(a, a.o_stride, a.channels)) return TCR_ERR_INVALID_ARG;
         // (other workgroups read what one has written out for: b and c, and in the states' kernel all of them)
         const Extent written = extent(a, out, a.o_stride, a.channels, size);
-        if (share(written, extent(a, x, a.x_stride, a.channels, size)) || share(written, extent(a, dt, a.dt_stride, a.channels, size)) ||
-            share(written, extent(a, b, a.b_stride, a.states, size, a.groups)) || share(written, extent(a, c, a.c_stride, a.states, size, a.groups)) ||
-            (gate != nullptr && share(written, extent(a, gate, a.gate_stride, a.channels, size))))
-            return TCR_ERR_INVALID_ARG;
+        if (share(written, state, bytes) || share(written, last, bytes)) return TCR_ERR_INVALID_ARG;
+        for (const Extent& read : {extent(a, x, a.x_stride, a.channels, size), extent(a, dt, a.dt_stride, a.channels, size), extent(a, b, a.b_stride, a.states, size, a.groups),
+                                   extent(a, c, a.c_stride, a.states, size, a.groups), extent(a, gate, a.gate_stride, a.channels, size)})
+            if (read.from != 0 && (share(written, read) || (!one && share(read, last, bytes)))) return TCR_ERR_INVALID_ARG;
     }
-    const uint64_t bytes = 4 * a.sequences * (uint64_t)a.channels * a.states;
     if ((state != last || !one) && arrays_share(state, bytes, last, bytes)) return TCR_ERR_INVALID_ARG;
     Selective s = arguments(a, x, dt, b, c, gate);
     s.out = out;
