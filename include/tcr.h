@@ -365,7 +365,8 @@ tcr_status tcr_selective_scan_step(const tcr_selective *shape, const void *x, co
 /*
  * Gradients of tcr_selective_scan.  dout is laid out by o_stride; dx, ddt, dgate (NULL where gate is) are contiguous (sequence, token, channel -- packed: token, channel),
  * db and dc (sequence, token, group, state), summed over a group's channels; da, dskip, ddt_bias (NULL: not wanted) like a, skip and dt_bias, summed over all tokens: the
- * same from run to run.  None of them stands in an input's place (not checked but for dstate).  state: the forward call's; dfinal: the gradient of its final_state (NULL: none);
+ * same from run to run.  None of them stands in an input's place (not checked but for dstate).  An infinity or NaN of a token or state
+ * reaches the gradients of its own sequence only, and the sums over all tokens (da, dskip, ddt_bias).  state: the forward call's; dfinal: the gradient of its final_state (NULL: none);
  * dstate: the gradient of `state` (NULL: not wanted).  Takes up to 6, 6, 7, 17 or 49 bytes of workspace for each token and channel with up to 4, 8, 16, 32 or 64 states, the
  * channels of each group rounded up to a multiple of 256, 128, 64, 32 or 16, and as much as for 32 tokens more for each sequence; of a caller's buffer that is the second half of what
  * follows its first 256 bytes.  With less TCR_ERR_WORKSPACE, or TCR_ERR_UNSUPPORTED where the stream is being recorded, and nothing done.
@@ -378,8 +379,8 @@ tcr_status tcr_selective_scan_backward(const tcr_selective *shape, const void *d
  * The Euclidean norm of many tensors together -- the gradients of a model -- and their scaling to a largest norm:
  *   norm[0] = sqrt(sum of the squares of all elements),   out = min(1, max_norm / (norm + eps)) * element.
  * tensors: `count` of them, in HOST memory (read during the call); data: DEVICE pointer to `count` consecutive elements of type dtype (TCR_F16, TCR_BF16,
- * TCR_F32), element aligned.  norm: one float on the device.  Sums are binary64, scaled elements rounded once; results are the same from run to run.  No tensors, or
- * empty ones: 0.  An infinity or NaN among them makes the norm infinite or NaN, and what is scaled 0 (the infinity itself NaN) or NaN.
+ * TCR_F32), element aligned.  norm: one float on the device.  Sums and the quotient are binary64; the factor is rounded to binary32, its products to binary32 and then to the type;
+ * results are the same from run to run.  No tensors, or empty ones: 0.  An infinity or NaN among them makes the norm infinite or NaN, and what is scaled 0 (the infinity itself NaN) or NaN.
  * out: HOST array of `count` DEVICE pointers, where the scaled tensors go; NULL: in place.  Where the factor is 1, tensors in place are not written.  What is written
  * stands in no other tensor's place and only once in the list (TCR_ERR_INVALID_ARG).  max_norm, eps >= 0.  At most 2^40 elements.
  * Takes 64 KiB of workspace, or 8 bytes for each 143 tensors where that is more, less where the tensors are few and small; of a caller's buffer that is the second half of what follows its

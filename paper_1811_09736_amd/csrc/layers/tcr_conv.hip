@@ -15,8 +15,9 @@ constexpr uint32_t kMostChannels = 1u << 20;
 // Threads that a call is cut for, and tokens of a run at most (the W - 1 in front of it are loaded once more).
 constexpr uint64_t kFillThreads = 1u << 18;
 constexpr uint32_t kLongRun = 32, kShortRun = 4;
-// Workgroups of the gradients: three for each compute unit, which are there at once (165 registers), each with runs as long as it takes.  8191 tokens x 4096 channels: 55 us, and 5 for the
-// sums; with four workgroups, of which one waits for the others, 62 and 6.
+// Workgroups of the gradients: three for each compute unit, which with four taps in 16 bits are there at once (165 registers), each with runs as long as it takes.  8191 tokens x 4096 channels:
+// 55 us, and 5 for the sums; with four workgroups, of which one waits for the others, 62 and 6.  (Four taps in binary32 take 180 registers and have two there at once, two taps in 16 bits
+// would have four.  Runs of every sequence are rounded up by themselves, and workgroups by the slabs of channels, so that a few may be left for a second turn.  Neither was measured.)
 constexpr uint64_t kGradBlocks = 768;
 
 uint64_t spans_of(const Conv& a) { return a.offsets != nullptr ? 1 : a.sequences; }

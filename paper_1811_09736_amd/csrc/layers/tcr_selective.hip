@@ -8,8 +8,9 @@ using tcr::host::partials_for;
 
 namespace {
 
-// Wavefronts that a scan is cut for -- four on each SIMD: 8192 tokens x 4096 channels x 16 states 272 us, with two 325, with eight 274 -- and chunks of a sequence at
-// most: each looks through the ones in front of it.
+// Wavefronts that a scan is cut for -- four on each SIMD: 8192 tokens x 4096 channels x 16 states, bfloat16, 272 us, with two 325, with eight 274 -- and chunks of a sequence at
+// most: each looks through the ones in front of it.  Four is what the output kernels' registers allow in 16 bits up to 16 states; with more states, and in binary32 from 8, three, with 64 two
+// or one, and channels that do not divide 1024 workgroups leave a few over: the last ones start when others have ended.  (Only the case above was measured.)
 constexpr uint64_t kFillWaves = 4096, kMostChunks = 64;
 
 template <typename T, int K, int P>

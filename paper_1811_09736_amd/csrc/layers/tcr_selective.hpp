@@ -138,7 +138,7 @@ struct Slab {
 };
 
 // Of the wavefronts of a SIMD the one that is ahead waits: left to itself the oldest runs first, and the last ones alone at the end, when one wavefront by itself
-// issues half as fast as two.  A step's priority is one less than that of the step in front of it, around four.  (8192 tokens x 4096 channels: 168 + 124 us without, 156 + 116 with.)
+// issues half as fast as two.  A step's priority is one less than that of the step in front of it, around four.  (8192 tokens x 4096 channels, the two kernels under rocprofv3: 168 + 124 us without, 156 + 116 with.)
 __device__ __forceinline__ void keep_pace(uint32_t step) {
     switch (step & 3) {
         case 0: __builtin_amdgcn_s_setprio(3); break;
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(kScanThreads) void selective_kernel(Selective s, ui
 }
 
 // One token for every sequence: four states a lane, P lanes a channel, lane = channel * P + part as the states lie in memory; S sequences a thread, all loads first.
-// Bound by the states' bytes, which pass the caches by: the next step finds none of them there (256 sequences x 4096 channels x 16 states 34 us, 4.2 TB/s; kept in the caches 42).
+// Bound by the states' bytes, which pass the caches by: the next step finds none of them there (256 sequences x 4096 channels x 16 states 33 us, 4.3 TB/s; kept in the caches 42).
 template <typename T, int P, int S>
 __global__ __launch_bounds__(kScanThreads) void selective_step_kernel(Selective s, uint32_t whole) {
     constexpr int K = 4, kChannels = kScanThreads / P;
